@@ -221,6 +221,89 @@ int32_t d3_n_ctx(const d3_ctx *ctx);
  * lies above every sequence's first row). */
 int d3_truncate(d3_ctx *ctx, int32_t n_rows);
 
+/* ---- A paged key-value cache ----------------------------------------------------------------------------------
+ * The context's own cache gives every sequence max_seq rows and the batch one common row count.  Here sequences (the
+ * batches of Section 4.2, as a server has them) come, grow and end one by one: their rows lie in pages of page_rows rows,
+ * listed in a table per sequence, and every sequence has a length of its own.  All state is in caller-owned device memory and
+ * is read by the kernels, so that the calls below, which allocate nothing and wait for nothing, can be captured into a HIP graph
+ * and replayed while the sequences grow:
+ *   tables      int32 [max_batch][max_pages]: the pages of each sequence in order; entries past its rows are not read;
+ *   rows        int32 [max_batch]: rows of each sequence (clamped to [0, max_pages * page_rows]); 0: none;
+ *   free_pages  int32 [n_pages], n_free int32 [2]: a stack of the pages that no sequence has, the last of the first
+ *               n_free[0] entries on top, and how many pages the last d3_pages_reserve lacked (n_free[1]);
+ *   slots       int32: where rows go, page * page_rows + row.
+ * k_pages, v_pages: dev, a pool of n_pages pages per layer, of kv_dtype; every page holds page_rows rows of each KV head:
+ *   K [layer][page][H_kv][page_rows][head_dim]
+ *   V [layer][page][H_kv][page_rows / R][head_dim][R], R = 8 (D3_F16) or 4 (D3_F32) consecutive rows of one dim in 16 bytes,
+ * as the matrix cores take them.  Values are clamped to +-65504 in D3_F16 pools; NaN stays.  A page number outside
+ * [0, n_pages) in a table is a page that is not there: its rows count as masked.  A slot outside the pool is skipped.
+ * A row may be given to one slot at a time (two rows of one call with the same slot: either is kept, element by element).
+ * Calls on one d3_pages must be ordered (one stream, or streams that wait for each other; replays of graphs too): they share
+ * its workspace, and they read what the ones before wrote. */
+typedef struct {
+    int32_t n_layers, n_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128; n_heads % n_kv_heads == 0 */
+    int32_t kv_dtype;                                  /* D3_F16 or D3_F32, see d3_model_desc */
+    int32_t n_pages, page_rows;                        /* page_rows: a power of two in [16, 1024]; n_pages * page_rows < 2^31 */
+    int32_t max_batch, max_pages;                      /* sequences (at most 4096); pages of one (max_pages * page_rows <= 2^30); max_batch * max_pages < 2^31 */
+} d3_pages_desc;
+
+typedef struct d3_pages d3_pages;
+
+/* Bytes of device workspace of a d3_pages (0 on a bad desc): the attention's partial results and counters. */
+size_t d3_pages_workspace_size(const d3_pages_desc *desc);
+
+/* Handle on caller-owned pools and workspace (256-byte aligned, d3_pages_workspace_size bytes; pools 16-byte aligned), on the current
+ * device, which the calls below make current for themselves.  Waits for the device once (it clears the counters). */
+int d3_pages_create(d3_pages **out, const d3_pages_desc *desc, void *k_pages, void *v_pages, void *workspace, size_t workspace_bytes);
+int d3_pages_destroy(d3_pages *pages);
+
+/* Page tables and slot maps from request lengths.  added: dev int32 [B]: how many rows sequence b asks for (0: none; negative: the sequence has
+ * ended, its pages go back and its rows become 0).  Pages of ended sequences are pushed first, in the order of b and of their tables.  Then the
+ * requests are granted in the order of b, whole or not at all: b is refused if its rows would pass max_pages * page_rows; else if the rows asked for
+ * up to and including it pass max_tokens; else if it needs pages and those needed up to and including it (by requests not refused so far for the other
+ * reasons) are more than there are.  Granted pages are popped in the order of b.
+ * Out: tables (entries of the granted pages), rows_out [B], starts [B + 1] (granted rows of the sequences before: sequence b's new rows are
+ * starts[b] .. starts[b + 1] - 1 of slots and positions; equal where nothing was granted), slots and positions [max_tokens] (cache slot, and row of the
+ * sequence, of every new row; -1 behind the last; positions may be NULL), n_free_out [2] (pages left; pages lacking).  rows_out may be rows_in and
+ * n_free_out may be n_free_in; kept apart, the same call can be made again. */
+int d3_pages_reserve(d3_pages *pages, int32_t B, const int32_t *added, const int32_t *rows_in, int32_t *rows_out, int32_t *tables,
+                     int32_t *free_pages, const int32_t *n_free_in, int32_t *n_free_out, int32_t max_tokens, int32_t *starts,
+                     int32_t *slots, int32_t *positions, void *hip_stream);
+
+/* Keys and values of n tokens into their slots of `n_layers` layers from `layer` on.  k, v: dev [n_layers][n][H_kv][head_dim] of `dtype` (any of d3_dtype),
+ * element (l, t, h, e) at l * layer_stride + t * token_stride + h * head_stride + e (strides in elements, multiples of 16 bytes; both pointers 16-byte aligned).  rope_cs: dev float
+ * [n][head_dim / 2][2], (cos, sin) of each token's angles, or NULL: keys turn by it (dims j and j + head_dim / 2 by angle j) before they are rounded once to the
+ * pool's type. */
+int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t *slots, const void *k, const void *v, int32_t dtype,
+                    int64_t token_stride, int64_t head_stride, int64_t layer_stride, const float *rope_cs, void *hip_stream);
+
+/* Attention of one token per sequence over its pages: out[b][h] = softmax(scale * q[b][h] . K^T) V over rows [0, rows[b]) of sequence b; 0 where it has no row.
+ * q, out: dev [B][n_heads][head_dim] of `dtype`, sequence b at b * q_stride, b * out_stride.  k_new, v_new: dev [B][H_kv][head_dim] of `dtype` at b * kv_stride, or both NULL.
+ * Given, they are row rows[b] - 1, which the call also writes to its page; else that row is there already.  rope_cs: dev float [B][head_dim / 2][2]: q and
+ * k_new turn by it; NULL: neither does.  q, k_new, v_new 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
+ * Keys and values are used as the pool holds them; sums and softmax in 32 bits. */
+int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,
+                       int64_t kv_stride, const float *rope_cs, const int32_t *tables, const int32_t *rows, float scale, void *out,
+                       int64_t out_stride, void *hip_stream);
+
+/* The missing-state fill on pages (D3_FILL_COPY, Section 3.2): rows `slots` of layer `src` are copied into layers [first, first + n_layers), which
+ * must not hold src; src < 0: zeros. */
+int d3_pages_fill(d3_pages *pages, int32_t n, const int32_t *slots, int32_t src, int32_t first, int32_t n_layers, void *hip_stream);
+
+/* Rows [row_begin, row_begin + n) of sequence `seq` of the context's own cache (counted from the sequence's first row if the batch was left-padded) into
+ * slots [n] of every layer: what a prompt pass wrote, into pages.  D3_ESHAPE unless the pages have the context's layers, KV heads and head_dim. */
+int d3_store_pages(d3_ctx *ctx, d3_pages *pages, int32_t seq, int32_t row_begin, int32_t n, const int32_t *slots, void *hip_stream);
+
+/* One decode step (as d3_decode_step) of B sequences whose rows are in `pages`: sequence b's token is row rows[b] - 1, for which d3_pages_reserve has made
+ * room, and its rotary position; a sequence without rows is idle (its tok_out and logits mean nothing).  Runs the blocks of step `step_i` of the plan, 0 <= step_i < n_steps, in any order
+ * of steps; the context's own cache, row count and step counter stay as they are.  D3_ESHAPE unless the pages have the context's shape and cache type;
+ * D3_ESTATE with D3_FILL_RECOMPUTE. */
+int d3_decode_step_paged(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, int32_t B, int32_t step_i, const int32_t *tables,
+                         const int32_t *rows, int32_t *tok_out, float *logits, float *hidden_dump, void *hip_stream);
+
+/* d3_pages_fill of the blocks that step `step_i` of the context's plan drops, from the block d3_fill_missing_kv takes (Section 3.2). */
+int d3_fill_missing_paged(d3_ctx *ctx, d3_pages *pages, int32_t step_i, int32_t n, const int32_t *slots, void *hip_stream);
+
 /* Measurement aid: per-launch timing of one kernel class with HIP events recorded
  * on the caller's stream (the projections dominate the step: its cost is that of
  * the decoder blocks it runs, Section 1).  While a class is

@@ -39,6 +39,10 @@ class _Weights(C.Structure):
     _fields_ = [("tok_emb", C.c_void_p), ("layers", C.POINTER(_LayerWeights)), ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
 
 
+class _PagesDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_heads", "n_kv_heads", "head_dim", "kv_dtype", "n_pages", "page_rows", "max_batch", "max_pages")]
+
+
 def library_path() -> str:
     return os.environ.get("D3_LIBRARY", os.path.join(_HERE, "libd3.so"))
 
@@ -76,6 +80,18 @@ def load_library() -> C.CDLL:
         lib.d3_n_ctx.restype = i32
         lib.d3_truncate.argtypes = [vp, i32]
         lib.d3_stream_read.argtypes = [vp, vp, C.c_size_t, vp]
+        i64 = C.c_int64
+        lib.d3_pages_workspace_size.argtypes = [C.POINTER(_PagesDesc)]
+        lib.d3_pages_workspace_size.restype = C.c_size_t
+        lib.d3_pages_create.argtypes = [C.POINTER(vp), C.POINTER(_PagesDesc), vp, vp, vp, C.c_size_t]
+        lib.d3_pages_destroy.argtypes = [vp]
+        lib.d3_pages_reserve.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+        lib.d3_pages_append.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, i64, i64, i64, vp, vp]
+        lib.d3_pages_attention.argtypes = [vp, i32, i32, vp, vp, vp, i32, i64, i64, vp, vp, vp, C.c_float, vp, i64, vp]
+        lib.d3_pages_fill.argtypes = [vp, i32, vp, i32, i32, i32, vp]
+        lib.d3_store_pages.argtypes = [vp, vp, i32, i32, i32, vp, vp]
+        lib.d3_decode_step_paged.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+        lib.d3_fill_missing_paged.argtypes = [vp, vp, i32, i32, vp, vp]
         lib.d3_mfma_yardstick.argtypes = [vp, i32, i32, vp]
         lib.d3_profile_select.argtypes = [vp, i32]
         lib.d3_profile_read.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
@@ -237,6 +253,24 @@ class Decoder:
     def set_fill_mode(self, mode: int) -> None:
         _check(self.lib.d3_set_fill_mode(self.ctx, mode))
 
+    def store_pages(self, cache: "PagedCache", seq: int, slots, row_begin: int = 0) -> None:
+        """Rows row_begin .. of sequence seq, as a prompt pass wrote them, into the slots (int32 CUDA tensor) of every layer of `cache`."""
+        cache._ints(slots=slots)
+        _check(self.lib.d3_store_pages(self.ctx, cache.handle, seq, row_begin, slots.numel(), slots.data_ptr(), self._stream()))
+
+    def decode_step_paged(self, cache: "PagedCache", tok_in, step_i: int, tok_out, logits=None, hidden_dump=None) -> None:
+        """One step of the cache's first tok_in.numel() sequences, whose newest rows cache.reserve has made room for."""
+        cache._ints(tok_in=tok_in, tok_out=tok_out)
+        if tok_out.numel() < tok_in.numel():
+            raise ValueError("tok_out is shorter than tok_in")
+        _check(self.lib.d3_decode_step_paged(self.ctx, cache.handle, tok_in.data_ptr(), tok_in.numel(), step_i, cache.tables.data_ptr(),
+                                             cache.rows.data_ptr(), tok_out.data_ptr(), _ptr(logits), _ptr(hidden_dump), self._stream()))
+
+    def fill_missing_paged(self, cache: "PagedCache", slots, step_i: int) -> None:
+        """COPY fill of the rows `slots` in the blocks that step step_i of the plan drops."""
+        cache._ints(slots=slots)
+        _check(self.lib.d3_fill_missing_paged(self.ctx, cache.handle, step_i, slots.numel(), slots.data_ptr(), self._stream()))
+
     def synchronize(self) -> None:
         self.torch.cuda.current_stream(self.device).synchronize()
 
@@ -264,6 +298,150 @@ class Decoder:
     @property
     def n_ctx(self) -> int:
         return int(self.lib.d3_n_ctx(self.ctx))
+
+
+class PagedCache:
+    """A paged key-value cache (the d3_pages_* entry points) and the operators on it: one handle, the page pools and the
+    state of the sequences, all torch tensors on one GPU.  Every call is asynchronous on the current stream, allocates nothing on the
+    device unless an output is left out, and can be captured into a graph.
+
+    k_pages [n_layers][n_pages][n_kv_heads][page_rows][head_dim] and v_pages [n_layers][n_pages][n_kv_heads][page_rows / R][head_dim][R]
+    (R = 8 for "f16", 4 for "f32"); tables int32 [max_batch][max_pages]; rows int32 [max_batch]; free_pages int32 [n_pages], a stack of which
+    the first n_free[0] entries count.  Buffers that are not given are made: pools of zeros, no sequences, all pages free."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, page_rows: int, max_batch: int, max_pages: int,
+                 kv_dtype: str = "f16", n_layers: int = 1, k_pages=None, v_pages=None, tables=None, rows=None, free_pages=None, n_free=None,
+                 device: str = "cuda:0"):
+        import torch
+        self.torch = torch
+        self.lib = load_library()
+        self.handle = None
+        self.device = torch.device(device)
+        self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim = n_layers, n_heads, n_kv_heads, head_dim
+        self.n_pages, self.page_rows, self.max_batch, self.max_pages, self.kv_dtype = n_pages, page_rows, max_batch, max_pages, kv_dtype
+        kinds = {"f32": D3_F32, "bf16": D3_BF16, "f16": D3_F16}
+        if kv_dtype not in kinds:
+            raise ValueError(f"kv_dtype must be one of {sorted(kinds)} (got {kv_dtype!r})")
+        desc = _PagesDesc(n_layers, n_heads, n_kv_heads, head_dim, kinds[kv_dtype], n_pages, page_rows, max_batch, max_pages)
+        ws_bytes = int(self.lib.d3_pages_workspace_size(C.byref(desc)))
+        if ws_bytes == 0:
+            raise D3Error(-2, self.lib.d3_last_error().decode())
+        self._kinds = {torch.float32: D3_F32, torch.bfloat16: D3_BF16, torch.float16: D3_F16}
+        tdt = {"f32": torch.float32, "f16": torch.float16}[kv_dtype]
+        unit = 16 // tdt.itemsize
+        with torch.cuda.device(self.device):
+            def buffer(name, given, dims, dtype, make):
+                if given is None:
+                    return make(dims, dtype=dtype, device=self.device)
+                if tuple(given.shape) != tuple(dims) or given.dtype != dtype or given.device != self.device or not given.is_contiguous():
+                    raise ValueError(f"{name} must be a contiguous {dtype} tensor {tuple(dims)} on {self.device}")
+                return given
+            self.k_pages = buffer("k_pages", k_pages, (n_layers, n_pages, n_kv_heads, page_rows, head_dim), tdt, torch.zeros)
+            self.v_pages = buffer("v_pages", v_pages, (n_layers, n_pages, n_kv_heads, page_rows // unit, head_dim, unit), tdt, torch.zeros)
+            none = lambda dims, **kw: torch.full(dims, -1, **kw)
+            self.tables = buffer("tables", tables, (max_batch, max_pages), torch.int32, none)
+            self.rows = buffer("rows", rows, (max_batch,), torch.int32, torch.zeros)
+            self.free_pages = buffer("free_pages", free_pages, (n_pages,), torch.int32, lambda dims, **kw: torch.arange(n_pages - 1, -1, -1, **kw))
+            self.n_free = buffer("n_free", n_free, (2,), torch.int32, lambda dims, **kw: torch.tensor([n_pages, 0], **kw))
+            self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+            handle = C.c_void_p()
+            _check(self.lib.d3_pages_create(C.byref(handle), C.byref(desc), self.k_pages.data_ptr(), self.v_pages.data_ptr(),
+                                            self.workspace.data_ptr(), ws_bytes))
+        self.handle = handle
+
+    def close(self) -> None:
+        if getattr(self, "handle", None):
+            self.lib.d3_pages_destroy(self.handle)
+            self.handle = None
+
+    __del__ = close
+
+    def _stream(self) -> int:
+        return self.torch.cuda.current_stream(self.device).cuda_stream
+
+    def _ints(self, **tensors) -> None:
+        for name, t in tensors.items():
+            if t.dtype != self.torch.int32 or t.device != self.device or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous int32 tensor on {self.device}")
+
+    def _angles(self, rope_cs, n: int) -> Optional[int]:
+        if rope_cs is None:
+            return None
+        if rope_cs.dtype != self.torch.float32 or rope_cs.device != self.device or not rope_cs.is_contiguous() or tuple(rope_cs.shape) != (n, self.head_dim // 2, 2):
+            raise ValueError(f"rope_cs must be a contiguous float32 tensor ({n}, {self.head_dim // 2}, 2) on {self.device}")
+        return rope_cs.data_ptr()
+
+    def _heads(self, name: str, t, dims):
+        """The tensor's dtype as d3_dtype; its last dim must be dense."""
+        if tuple(t.shape) != tuple(dims) or t.device != self.device or t.dtype not in self._kinds or t.stride(-1) != 1:
+            raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor {tuple(dims)} on {self.device} whose last dim is dense")
+        return self._kinds[t.dtype]
+
+    def reserve(self, added, max_tokens: int, starts=None, slots=None, positions=None, rows_out=None, n_free_out=None):
+        """Room for added[b] more rows of sequence b (int32 CUDA tensor [B]; 0: none, negative: the sequence has ended), B <= max_batch, at most max_tokens rows in all.
+        Updates tables, rows and the stack of free pages (rows_out [B] and n_free_out [2]: elsewhere than in place) and returns (starts [B + 1], slots [max_tokens],
+        positions [max_tokens]): sequence b's new rows are entries starts[b] .. starts[b + 1] - 1 of the other two, none where the request was refused."""
+        torch, B = self.torch, added.numel()
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=self.device)
+        if B > self.max_batch or max_tokens < 0:
+            raise ValueError(f"added must have at most {self.max_batch} entries and max_tokens must not be negative")
+        starts = new(B + 1) if starts is None else starts
+        slots = new(max_tokens) if slots is None else slots
+        positions = new(max_tokens) if positions is None else positions
+        rows_out = self.rows if rows_out is None else rows_out
+        n_free_out = self.n_free if n_free_out is None else n_free_out
+        self._ints(added=added, starts=starts, slots=slots, positions=positions, rows_out=rows_out, n_free_out=n_free_out)
+        if starts.numel() < B + 1 or slots.numel() < max_tokens or positions.numel() < max_tokens or rows_out.numel() < B or n_free_out.numel() < 2:
+            raise ValueError("an output is shorter than what reserve writes")
+        _check(self.lib.d3_pages_reserve(self.handle, B, added.data_ptr(), self.rows.data_ptr(), rows_out.data_ptr(), self.tables.data_ptr(),
+                                         self.free_pages.data_ptr(), self.n_free.data_ptr(), n_free_out.data_ptr(), max_tokens, starts.data_ptr(),
+                                         slots.data_ptr(), positions.data_ptr(), self._stream()))
+        return starts, slots, positions
+
+    def append(self, layer: int, slots, k, v, rope_cs=None) -> None:
+        """k, v [n][n_kv_heads][head_dim], or [m][n][n_kv_heads][head_dim] for the m layers from `layer` on, into the rows `slots` (int32 CUDA tensor [n]) of the pools.
+        rope_cs [n][head_dim / 2][2]: (cos, sin) by which the keys turn first."""
+        if k.dim() == 3:
+            k, v = k[None], v[None]
+        n, layers = slots.numel(), k.shape[0]
+        dims = (layers, n, self.n_kv_heads, self.head_dim)
+        kind = self._heads("k", k, dims)
+        self._heads("v", v, dims)
+        self._ints(slots=slots)
+        if k.dtype != v.dtype or k.stride() != v.stride():
+            raise ValueError("k and v must have one dtype and the same strides")
+        _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, k.stride(1), k.stride(2), k.stride(0),
+                                        self._angles(rope_cs, n), self._stream()))
+
+    def attend(self, layer: int, q, k=None, v=None, rope_cs=None, scale: float = 0.0, out=None):
+        """Attention of one token of each of the first B sequences, q [B][n_heads][head_dim], over their rows; returns out [B][n_heads][head_dim] of q's dtype.
+        k, v [B][n_kv_heads][head_dim]: the newest rows (row rows[b] - 1), which the call also writes to their pages; without them they are there already.
+        rope_cs [B][head_dim / 2][2]: q and k turn by it.  scale 0: 1 / sqrt(head_dim)."""
+        B = q.shape[0]
+        dims = (B, self.n_heads, self.head_dim)
+        kind = self._heads("q", q, dims)
+        if out is None:
+            out = self.torch.empty(dims, dtype=q.dtype, device=self.device)
+        self._heads("out", out, dims)
+        if out.dtype != q.dtype or q.stride(1) != self.head_dim or out.stride(1) != self.head_dim:
+            raise ValueError("q and out must have one dtype and the heads of a sequence side by side")
+        if (k is None) != (v is None):
+            raise ValueError("k and v come together or not at all")
+        kv_stride = 0
+        if k is not None:
+            self._heads("k", k, (B, self.n_kv_heads, self.head_dim))
+            self._heads("v", v, (B, self.n_kv_heads, self.head_dim))
+            if k.dtype != q.dtype or v.dtype != q.dtype or k.stride() != v.stride() or k.stride(1) != self.head_dim:
+                raise ValueError("k and v must have q's dtype, the same strides and the heads of a sequence side by side")
+            kv_stride = k.stride(0)
+        _check(self.lib.d3_pages_attention(self.handle, layer, B, q.data_ptr(), _ptr(k), _ptr(v), kind, q.stride(0), kv_stride, self._angles(rope_cs, B),
+                                           self.tables.data_ptr(), self.rows.data_ptr(), scale, out.data_ptr(), out.stride(0), self._stream()))
+        return out
+
+    def fill(self, slots, src: int, first: int, n_layers: int) -> None:
+        """Rows `slots` of layer src (zeros if negative) copied into layers first .. first + n_layers - 1."""
+        self._ints(slots=slots)
+        _check(self.lib.d3_pages_fill(self.handle, slots.numel(), slots.data_ptr(), src, first, n_layers, self._stream()))
 
 
 def weights_to_device(shape, weights_np: Dict[str, object], device: str = "cuda:0") -> Dict[str, object]:

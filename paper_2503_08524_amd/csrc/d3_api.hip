@@ -12,6 +12,7 @@
 #include "../../include/d3.h"
 #include "d3_common.h"
 #include "d3_error.h"
+#include "pages.h"
 
 using namespace d3;
 
@@ -448,17 +449,22 @@ bool whole_context_attention(const d3_ctx* c, const SeqRuns& runs, bool shared) 
     return std::max(2.85 * longest, 3.3 * steps / c->n_cu) <= tiles_us;
 }
 
+// A decode pass whose sequences' rows are in pages instead of the context's cache.
+struct Paged { const d3_pages* pages; const int32_t *tables, *rows; };
+
 // One pass of `ncols` columns through the listed blocks.  hidden_dump (or NULL): dev
 // [(n_ids+1)][dump_cols][d], fed from columns [dump_first, dump_first + dump_cols).
 // shared: a prompt pass whose columns are runs of several sequences (cm then gives P and
 // pos_begin only, and there is no head); picks: its last positions, which hidden_dump takes.
 // fp32_projections: fp32 activations on the vector ALUs also where the pass has several columns.
 // cut_len > 0: the context's splits are so many rows long, instead of as the pass's columns would have them.
+// paged: column c is sequence c's newest row in these pages (cm then says nothing but that every column is a sequence).
 // save_before >= 0: the residual that enters the first listed block >= save_before (the one after the last, if none)
 // is copied to the workspace's h_skip: it is what the blocks of the drop window would have seen.
 int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_t* ids, int n_ids,
             float* hidden_dump, int dump_first, int dump_cols, const HeadOut* head, hipStream_t s, int save_before = -1,
-            int dump_total = -1, int dump_dst = 0, const SeqRuns* shared = nullptr, const RowPick* picks = nullptr, bool fp32_projections = false, int cut_len = 0) {
+            int dump_total = -1, int dump_dst = 0, const SeqRuns* shared = nullptr, const RowPick* picks = nullptr, bool fp32_projections = false, int cut_len = 0,
+            const Paged* paged = nullptr) {
     const d3_model_desc& d = c->desc;
     const int dm = d.d_model, hd = d.head_dim, qdim = d.n_heads * hd, kvdim = d.n_kv_heads * hd, qkv_dim = qdim + 2 * kvdim, F = d.d_ffn;
     float* x = c->at<float>(c->lay.x);
@@ -487,7 +493,7 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
 
     // a prompt chunk of one sequence (consecutive positions) or of several: tiles of queries share the cache rows they read
     const int grp = d.n_heads / d.n_kv_heads;
-    const bool qtile = shared || (c->prefill_by_seq && mfma && cm.B == 1 && ncols >= 2 && hd == 128 &&
+    const bool qtile = shared || (!paged && c->prefill_by_seq && mfma && cm.B == 1 && ncols >= 2 && hd == 128 &&
                                   (grp == 1 || grp == 2 || grp == 4 || grp == 8));
     SeqRuns one{};
     one.n = 1; one.seq[0] = cm.seq(0); one.col[1] = ncols; one.pos[0] = cm.pos(0);
@@ -499,7 +505,8 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
     auto form = [&](int K) { return lines ? split_lines() : split_planes(K, c->lay.split_cols); };
     const EmbedSplit split{mfma ? gain_after(-1) : nullptr, n_split, ssq, form(dm)};
     int2* col_at = qtile ? c->at<int2>(c->lay.col_at) : nullptr;
-    if (qtile) D3_HIP(launch_embed_runs(c->tok_emb, tokens, runs, cm.P, cm.pos_begin, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, row0, col_at, split, s));
+    if (paged) D3_HIP(launch_embed_paged(c->tok_emb, d.weight_dtype, tokens, paged->rows, paged->pages->desc.max_pages * paged->pages->desc.page_rows, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, split, s));
+    else if (qtile) D3_HIP(launch_embed_runs(c->tok_emb, tokens, runs, cm.P, cm.pos_begin, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, row0, col_at, split, s));
     else D3_HIP(launch_embed(c->tok_emb, d.weight_dtype, tokens, cm, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, row0, split, s));
     auto dump = [&](int slot) -> int {
         if (!hidden_dump) return 0;
@@ -516,7 +523,7 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
     int split_len = 0, n_splits = 0;
     const int context = cm.pos(ncols - 1) + 1;
     if (cut_len > 0) { split_len = cut_len; n_splits = (context + cut_len - 1) / cut_len; }
-    else if (!prompt_attn && !shared) pick_splits(c, ncols, context, c->attn_wgs_per_cu * c->n_cu, &split_len, &n_splits, qtile);
+    else if (!prompt_attn && !shared && !paged) pick_splits(c, ncols, context, c->attn_wgs_per_cu * c->n_cu, &split_len, &n_splits, qtile);
 
     bool saved = save_before < 0;
     auto save_skip = [&]() -> int {
@@ -570,7 +577,15 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
         at.rope_cs = rope_in_attn ? rope_cs : nullptr;
         at.qtile = qtile ? 1 : 0;
         at.row0 = row0;
-        if (shared && !prompt_attn) {
+        if (paged) {
+            PagedAttnArgs pa = paged_attn_args(paged->pages, l, ncols);
+            pa.q = qkv; pa.k_new = qkv + qdim; pa.v_new = qkv + qdim + kvdim; pa.dtype = D3_F32;
+            pa.q_stride = qkv_dim; pa.kv_stride = qkv_dim; pa.out_stride = qdim;
+            pa.rope_cs = rope_cs; pa.tables = paged->tables; pa.rows = paged->rows;
+            pa.out = at.out; pa.out_split = at.out_split; pa.out_form = at.out_form;
+            Timed t(c, D3_K_ATTN, s);
+            D3_HIP(launch_attention_paged(pa, hd, d.kv_dtype, c->n_cu, s));
+        } else if (shared && !prompt_attn) {
             for (int r = 0; r < runs.n; ++r) {         // one after the other: the partials and the counters are the launch's own
                 const int col = runs.col[r];
                 AttnArgs own = at;
@@ -914,6 +929,65 @@ extern "C" int d3_decode_step(d3_ctx* ctx, const int32_t* tok_in, int32_t step_i
 extern "C" int d3_decode_step_static(d3_ctx* ctx, const int32_t* tok_in, int32_t step_i, int32_t* tok_out, float* logits,
                                      float* hidden_dump, void* hip_stream) {
     return decode_step_impl(ctx, tok_in, step_i, tok_out, logits, hidden_dump, static_cast<hipStream_t>(hip_stream), true);
+}
+
+namespace {
+
+// The pages are of the context's shape and on its GPU.
+int check_pages(const d3_ctx* ctx, const d3_pages* pages, const char* who, bool same_type) {
+    const d3_model_desc& d = ctx->desc;
+    const d3_pages_desc& p = pages->desc;
+    if (p.n_layers != d.n_layers || p.n_heads != d.n_heads || p.n_kv_heads != d.n_kv_heads || p.head_dim != d.head_dim || (same_type && p.kv_dtype != d.kv_dtype))
+        return fail(D3_ESHAPE, "%s: the pages' layers, heads, head_dim%s must be the context's", who, same_type ? " and type" : "");
+    if (pages->dev != ctx->dev) return fail(D3_EINVAL, "%s: the pages are on device %d, the context on %d", who, pages->dev, ctx->dev);
+    return D3_OK;
+}
+
+}  // namespace
+
+extern "C" int d3_decode_step_paged(d3_ctx* ctx, d3_pages* pages, const int32_t* tok_in, int32_t B, int32_t step_i, const int32_t* tables,
+                                    const int32_t* rows, int32_t* tok_out, float* logits, float* hidden_dump, void* hip_stream) {
+    if (!ctx || !pages || !tok_in || !tables || !rows || !tok_out) return fail(D3_EINVAL, "d3_decode_step_paged: NULL argument");
+    int rc = check_pages(ctx, pages, "d3_decode_step_paged", true);
+    if (rc != D3_OK) return rc;
+    if (!ctx->has_plan) return fail(D3_ESTATE, "d3_decode_step_paged: no plan set (call d3_set_plan)");
+    if (step_i < 0 || step_i >= ctx->n_steps) return fail(D3_ERANGE, "d3_decode_step_paged: step %d is outside the plan of %d steps", step_i, ctx->n_steps);
+    const int most = std::min(ctx->desc.max_batch, pages->desc.max_batch);
+    if (B < 1 || B > most) return fail(D3_ESHAPE, "d3_decode_step_paged: B must be in [1, %d] (got %d)", most, B);
+    if (ctx->fill_mode == D3_FILL_RECOMPUTE)                    // that fill reads what the latest step on the context's own cache left in the workspace
+        return fail(D3_ESTATE, "d3_decode_step_paged: the RECOMPUTE fill is of the context's own cache");
+    const OnDevice on(ctx->dev);
+    const Paged paged{pages, tables, rows};
+    const ColMap cm{0, B, 1, 0};
+    const HeadOut head{0, B, logits ? logits : ctx->at<float>(ctx->lay.logits), tok_out};
+    return forward(ctx, tok_in, cm, B, ctx->layer_ids.data() + (size_t)step_i * ctx->desc.n_layers, ctx->keep[step_i], hidden_dump, 0, B, &head,
+                   static_cast<hipStream_t>(hip_stream), -1, -1, 0, nullptr, nullptr, false, 0, &paged);
+}
+
+extern "C" int d3_store_pages(d3_ctx* ctx, d3_pages* pages, int32_t seq, int32_t row_begin, int32_t n, const int32_t* slots, void* hip_stream) {
+    if (!ctx || !pages) return fail(D3_EINVAL, "d3_store_pages: NULL argument");
+    int rc = check_pages(ctx, pages, "d3_store_pages", false);
+    if (rc != D3_OK) return rc;
+    if (!ctx->prefilled) return fail(D3_ESTATE, "d3_store_pages: no prompt pass yet (call d3_prefill)");
+    if (seq < 0 || seq >= ctx->B) return fail(D3_ERANGE, "d3_store_pages: sequence %d is outside the batch of %d", seq, ctx->B);
+    const int first = ctx->ragged ? ctx->row0[seq] : 0, held = ctx->n_ctx - first;
+    if (row_begin < 0 || n < 0 || n > held - row_begin) return fail(D3_ERANGE, "d3_store_pages: rows [%d, %d + %d) are outside the %d of the sequence", row_begin, row_begin, n, held);
+    if (n == 0) return D3_OK;
+    const d3_model_desc& d = ctx->desc;
+    const int es = kv_elem_bytes(d.kv_dtype);
+    const size_t at = (((size_t)seq * d.n_kv_heads) * d.max_seq + first + row_begin) * d.head_dim * es;
+    return d3_pages_append(pages, 0, d.n_layers, n, slots, ctx->k_cache + at, ctx->v_cache + at, d.kv_dtype, d.head_dim, (int64_t)d.max_seq * d.head_dim,
+                           (int64_t)(ctx->kv_layer_bytes() / es), nullptr, hip_stream);
+}
+
+extern "C" int d3_fill_missing_paged(d3_ctx* ctx, d3_pages* pages, int32_t step_i, int32_t n, const int32_t* slots, void* hip_stream) {
+    if (!ctx || !pages) return fail(D3_EINVAL, "d3_fill_missing_paged: NULL argument");
+    int rc = check_pages(ctx, pages, "d3_fill_missing_paged", false);
+    if (rc != D3_OK) return rc;
+    if (!ctx->has_plan) return fail(D3_ESTATE, "d3_fill_missing_paged: no plan set (call d3_set_plan)");
+    if (step_i < 0 || step_i >= ctx->n_steps) return fail(D3_ERANGE, "d3_fill_missing_paged: step %d is outside the plan of %d steps", step_i, ctx->n_steps);
+    const int L = ctx->desc.n_layers, first = ctx->drop_begin[step_i], dropped = L - ctx->keep[step_i];
+    return d3_pages_fill(pages, n, slots, first > 0 ? first - 1 : (first + dropped < L ? first + dropped : -1), first, dropped, hip_stream);
 }
 
 extern "C" size_t d3_static_scratch_bytes(void) { return kStaticScratchBytes; }

@@ -317,6 +317,10 @@ int launch_pick_rows(const float* x, int d, const RowPick& pick, float* dst, hip
 int launch_embed(const void* tok_emb, int weight_dtype, const int32_t* tokens, ColMap cm, int ncols, int d,
                  int vocab, float* x, const double* inv_freq, int half_hd, float2* rope_cs, const int* row0, const EmbedSplit& split, hipStream_t s);
 
+// A decode step on pages: sequence c's token is its row min(rows[c], max_rows) - 1.
+int launch_embed_paged(const void* tok_emb, int weight_dtype, const int32_t* tokens, const int32_t* rows, int max_rows, int ncols, int d, int vocab,
+                       float* x, const double* inv_freq, int half_hd, float2* rope_cs, const EmbedSplit& split, hipStream_t s);
+
 struct RopeArgs {
     float* qkv;            // [ncols][(H + 2 H_kv) * hd] fp32: q rotated in place
     void* k_cache;         // this block's [max_batch][H_kv][max_seq][hd]

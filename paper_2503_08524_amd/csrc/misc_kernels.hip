@@ -86,6 +86,13 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const bf16_t* __restric
     if (threadIdx.x == 0) col_at[c] = make_int2(seq, pos);
     embed_column<bf16_t>(emb, tokens[(size_t)seq * P + (pos - pos_begin)], pos - (row0 ? row0[seq] : 0), c, d, vocab, x, inv_freq, half_hd, rope_cs, split);
 }
+template <typename W>
+__global__ __launch_bounds__(256) void embed_paged_kernel(const W* __restrict__ emb, const int32_t* __restrict__ tokens, const int32_t* __restrict__ rows,
+                                                          int max_rows, int d, int vocab, float* __restrict__ x, const double* __restrict__ inv_freq, int half_hd,
+                                                          float2* __restrict__ rope_cs, EmbedSplit split) {
+    const int c = blockIdx.x;
+    embed_column<W>(emb, tokens[c], max(min(rows[c], max_rows) - 1, 0), c, d, vocab, x, inv_freq, half_hd, rope_cs, split);
+}
 
 // ---------------- the last positions of a prompt pass ----------------
 // dst may be the caller's hidden_dump, which is aligned to its floats and no more.
@@ -308,6 +315,17 @@ int launch_embed(const void* tok_emb, int weight_dtype, const int32_t* tokens, C
     else
         hipLaunchKernelGGL(embed_kernel<bf16_t>, dim3(ncols), dim3(256), 0, s, static_cast<const bf16_t*>(tok_emb), tokens, cm, d, vocab, x,
                            inv_freq, half_hd, rope_cs, row0, split);
+    return (int)hipGetLastError();
+}
+
+int launch_embed_paged(const void* tok_emb, int weight_dtype, const int32_t* tokens, const int32_t* rows, int max_rows, int ncols, int d, int vocab,
+                       float* x, const double* inv_freq, int half_hd, float2* rope_cs, const EmbedSplit& split, hipStream_t s) {
+    if (weight_dtype == 0)
+        hipLaunchKernelGGL(embed_paged_kernel<float>, dim3(ncols), dim3(256), 0, s, static_cast<const float*>(tok_emb), tokens, rows, max_rows, d, vocab, x,
+                           inv_freq, half_hd, rope_cs, split);
+    else
+        hipLaunchKernelGGL(embed_paged_kernel<bf16_t>, dim3(ncols), dim3(256), 0, s, static_cast<const bf16_t*>(tok_emb), tokens, rows, max_rows, d, vocab, x,
+                           inv_freq, half_hd, rope_cs, split);
     return (int)hipGetLastError();
 }
 

@@ -1,0 +1,311 @@
+// Kernels of the paged cache beside its attention: page tables and slot maps from request lengths, rows into pages, the missing-state fill on pages.
+#include <algorithm>
+
+#include "pages.h"
+
+namespace d3 {
+
+namespace {
+
+// ---------------- page tables and slot maps ----------------
+// One workgroup: sums over the sequences, each thread a few consecutive ones, then pages and tokens found in those sums by bisection.
+constexpr int kReserveThreads = 1024;
+constexpr int kSeqsPerThread = kPagesMaxSeqs / kReserveThreads;
+
+__device__ __forceinline__ unsigned long long shfl_up64(unsigned long long v, int o) {
+    const unsigned lo = __shfl_up((unsigned)v, o, 64), hi = __shfl_up((unsigned)(v >> 32), o, 64);
+    return (unsigned long long)hi << 32 | lo;
+}
+// Sum over the threads before this one, and over all; `red`: a word per wave, free again behind the next barrier but one.
+__device__ __forceinline__ unsigned long long scan_block(unsigned long long v, unsigned long long* red, unsigned long long* all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    unsigned long long s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const unsigned long long below = shfl_up64(s, o);
+        if (lane >= o) s += below;
+    }
+    if (lane == 63) red[wave] = s;
+    __syncthreads();
+    unsigned long long before = 0, sum = 0;
+    for (int w = 0; w < kReserveThreads / 64; ++w) {
+        if (w < wave) before += red[w];
+        sum += red[w];
+    }
+    *all = sum;
+    return before + s - v;
+}
+// the last of v[0 .. n - 1], not decreasing, that is at most x (v[0] is)
+__device__ __forceinline__ int last_at_most(const int* v, int n, int x) {
+    int lo = 0, hi = n - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (v[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// slot and position of new row t of the call; `tables` and `rows` as they are after it
+__device__ __forceinline__ void write_token(const ReserveArgs& a, const int* starts, int t) {
+    int slot = -1, p = -1;
+    if (t < starts[a.B]) {
+        const int b = last_at_most(starts, a.B, t);                 // sequences that got nothing share their start with the next one
+        p = a.rows_out[b] - starts[b + 1] + t;
+        const int page = a.tables[(size_t)b * a.max_pages + p / a.page_rows];
+        if ((unsigned)page < (unsigned)a.n_pages) slot = page * a.page_rows + p % a.page_rows;
+    }
+    a.slots[t] = slot;
+    if (a.positions) a.positions[t] = p;
+}
+
+__global__ __launch_bounds__(kReserveThreads) void pages_reserve_kernel(ReserveArgs a, int write_tokens) {
+    __shared__ int starts[kPagesMaxSeqs + 1], page_at[kPagesMaxSeqs + 1], back_at[kPagesMaxSeqs + 1], page_first[kPagesMaxSeqs];
+    __shared__ unsigned long long red[3][kReserveThreads / 64];
+    const int tid = threadIdx.x, b0 = tid * kSeqsPerThread, cap = a.max_pages * a.page_rows;
+    auto pages_of = [&](int rows) { return (int)(((unsigned)rows + a.page_rows - 1) / a.page_rows); };
+    int rows[kSeqsPerThread], need[kSeqsPerThread], back[kSeqsPerThread];
+    long long asked[kSeqsPerThread];
+    unsigned long long mine = 0, all;
+#pragma unroll
+    for (int j = 0; j < kSeqsPerThread; ++j) {
+        const int b = b0 + j;
+        const int add = b < a.B ? a.added[b] : 0;
+        rows[j] = b < a.B ? min(max(a.rows_in[b], 0), cap) : 0;
+        back[j] = add < 0 ? pages_of(rows[j]) : 0;
+        if (add < 0) rows[j] = 0;
+        asked[j] = add > 0 && (long long)rows[j] + add <= cap ? add : 0;
+        mine += asked[j];
+    }
+    // what of it fits max_tokens, the pages that needs, and the pages that come back: two sums in one word, neither passes 2^31
+    unsigned long long before = scan_block(mine, red[0], &all), both = 0;
+#pragma unroll
+    for (int j = 0; j < kSeqsPerThread; ++j) {
+        before += asked[j];
+        if (before > (unsigned long long)a.max_tokens) asked[j] = 0;
+        need[j] = pages_of(rows[j] + (int)asked[j]) - pages_of(rows[j]);
+        both += (unsigned long long)need[j] << 32 | (unsigned)back[j];
+    }
+    before = scan_block(both, red[1], &all);
+    const long long wanted = all >> 32, returned = (unsigned)all;
+    const int n_free = min(max(a.n_free_in[0], 0), a.n_pages), avail = (int)min((long long)n_free + returned, (long long)a.n_pages);
+    int need_before = (int)(before >> 32), back_before = (int)(unsigned)before;
+    both = 0;
+    int granted[kSeqsPerThread], first[kSeqsPerThread];
+#pragma unroll
+    for (int j = 0; j < kSeqsPerThread; ++j) {
+        first[j] = need_before;                                     // a refusal for pages refuses all behind it that need some: the sum is that of granted ones
+        granted[j] = need[j] == 0 || need_before + need[j] <= avail ? (int)asked[j] : 0;
+        need_before += need[j];
+        if (granted[j] == 0) need[j] = 0;
+        both += (unsigned long long)need[j] << 32 | (unsigned)granted[j];
+    }
+    before = scan_block(both, red[2], &all);
+    const int taken = (int)(all >> 32), tokens = (int)(unsigned)all;
+    int start = (int)(unsigned)before, page = (int)(before >> 32);
+#pragma unroll
+    for (int j = 0; j < kSeqsPerThread; ++j) {
+        const int b = b0 + j;
+        if (b >= a.B) break;
+        starts[b] = start; page_at[b] = page; back_at[b] = back_before;
+        page_first[b] = pages_of(rows[j]);
+        a.starts[b] = start;
+        a.rows_out[b] = rows[j] + granted[j];
+        start += granted[j]; page += need[j]; back_before += back[j];
+    }
+    if (tid == 0) {
+        starts[a.B] = tokens; page_at[a.B] = taken; back_at[a.B] = (int)returned;
+        a.starts[a.B] = tokens;
+    }
+    __syncthreads();                                                // (also: everybody has read n_free_in, which may be n_free_out)
+    if (tid == 0) {
+        a.n_free_out[0] = avail - taken;
+        a.n_free_out[1] = (int)max(wanted - avail, 0ll);
+    }
+    for (int x = tid; x < avail - n_free; x += kReserveThreads) {
+        const int b = last_at_most(back_at, a.B, x);
+        a.free_pages[n_free + x] = a.tables[(size_t)b * a.max_pages + x - back_at[b]];
+    }
+    __syncthreads();
+    for (int x = tid; x < taken; x += kReserveThreads) {
+        const int b = last_at_most(page_at, a.B, x);
+        a.tables[(size_t)b * a.max_pages + page_first[b] + x - page_at[b]] = a.free_pages[avail - 1 - x];
+    }
+    if (!write_tokens) return;
+    __syncthreads();
+    for (int t = tid; t < a.max_tokens; t += kReserveThreads) write_token(a, starts, t);
+}
+
+// the tokens alone, behind the kernel above
+__global__ __launch_bounds__(256) void pages_slots_kernel(ReserveArgs a) {
+    __shared__ int starts[kPagesMaxSeqs + 1];
+    for (int b = threadIdx.x; b <= a.B; b += 256) starts[b] = a.starts[b];
+    __syncthreads();
+    for (int t = blockIdx.x * 1024 + threadIdx.x; t < min(a.max_tokens, ((int)blockIdx.x + 1) * 1024); t += 256) write_token(a, starts, t);
+}
+
+// ---------------- rows into pages ----------------
+template <typename S> __device__ __forceinline__ void load8(const S* p, float (&y)[8]);
+template <> __device__ __forceinline__ void load8<float>(const float* p, float (&y)[8]) {
+    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+    y[0] = a.x; y[1] = a.y; y[2] = a.z; y[3] = a.w; y[4] = b.x; y[5] = b.y; y[6] = b.z; y[7] = b.w;
+}
+template <> __device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&y)[8]) {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    y[0] = bf16_lo(v.x); y[1] = bf16_hi(v.x); y[2] = bf16_lo(v.y); y[3] = bf16_hi(v.y);
+    y[4] = bf16_lo(v.z); y[5] = bf16_hi(v.z); y[6] = bf16_lo(v.w); y[7] = bf16_hi(v.w);
+}
+template <> __device__ __forceinline__ void load8<f16_t>(const f16_t* p, float (&y)[8]) {
+    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+    const half8 v = *reinterpret_cast<const half8*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = (float)v[e];
+}
+template <typename T> __device__ __forceinline__ void store8(T* p, const float (&y)[8]) {
+    alignas(16) T t[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) t[e] = held<T>(y[e]);
+#pragma unroll
+    for (int e = 0; e < 8; e += 16 / sizeof(T)) *reinterpret_cast<uint4*>(p + e) = *reinterpret_cast<const uint4*>(t + e);
+}
+
+// grid: (64 tokens, KV head, layer and half: keys or values).
+// A key is a row of its page; a value's dims lie 16 bytes apart, R rows side by side.  So values pass through LDS: the token that is
+// row 0 of a unit whose R rows all follow each other in `slots` writes the unit's 16 bytes per dim for all of them, and only rows
+// of units that the call does not fill are written element by element.  Tiles read R - 1 tokens of the next one, so that units across tiles are whole.
+constexpr int kAppendTokens = 64;
+
+template <typename S, typename T>
+__global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
+    constexpr int R = 16 / sizeof(T), TT = kAppendTokens;
+    __shared__ int slot_of[TT + 2 * (R - 1)];                      // of tokens t0 - (R - 1) .. t0 + TT + R - 2; -1: none
+    __shared__ __align__(16) T tile[(TT + R - 1) * 128];
+    const int tid = threadIdx.x, t0 = blockIdx.x * TT, h = blockIdx.y, layer = blockIdx.z >> 1, hd = a.hd, eighths = hd / 8;
+    const bool values = blockIdx.z & 1;
+    const S* src = static_cast<const S*>(values ? a.v : a.k) + layer * a.layer_stride + h * a.head_stride;
+    const size_t head_elems = (size_t)a.page_rows * hd;
+    auto pool_at = [&](void* pool, int slot) {                      // the head's rows of the slot's page
+        return reinterpret_cast<T*>(static_cast<char*>(pool) + layer * a.pool_bytes) + ((size_t)(slot / a.page_rows) * a.H_kv + h) * head_elems;
+    };
+    for (int x = tid; x < TT + 2 * (R - 1); x += 256) {
+        const int t = t0 - (R - 1) + x, slot = t >= 0 && t < a.n ? a.slots[t] : -1;
+        slot_of[x] = slot >= 0 && slot < a.n_slots ? slot : -1;
+    }
+    if (!values) {
+        __syncthreads();
+        const int pairs = hd / 16;                                 // a thread has eight dims of the lower half and their partners
+        for (int x = tid; x < TT * pairs; x += 256) {
+            const int t = x / pairs, j = x % pairs * 8, slot = slot_of[t + R - 1];
+            if (slot < 0) continue;
+            float lo[8], hi[8];
+            const S* row = src + (t0 + t) * a.token_stride;
+            load8<S>(row + j, lo);
+            load8<S>(row + j + hd / 2, hi);
+            if (a.rope_cs) {
+                const float2* cs = a.rope_cs + (size_t)(t0 + t) * (hd / 2) + j;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float2 c = cs[e];
+                    const float x0 = lo[e], x1 = hi[e];
+                    lo[e] = x0 * c.x - x1 * c.y;
+                    hi[e] = x1 * c.x + x0 * c.y;
+                }
+            }
+            T* to = pool_at(a.k_pages, slot) + slot % a.page_rows * hd + j;
+            store8<T>(to, lo);
+            store8<T>(to + hd / 2, hi);
+        }
+        return;
+    }
+    const int here = min(TT + R - 1, a.n - t0);
+    for (int x = tid; x < here * eighths; x += 256) {
+        const int t = x / eighths, j = x % eighths * 8;
+        float y[8];
+        load8<S>(src + (t0 + t) * a.token_stride + j, y);
+        store8<T>(tile + t * hd + j, y);
+    }
+    __syncthreads();
+    auto fills = [&](int x) {                                      // token x of slot_of is row 0 of a unit that R tokens in a row fill
+        bool all = x >= 0 && slot_of[x] >= 0 && slot_of[x] % R == 0;
+        for (int e = 1; e < R && all; ++e) all = slot_of[x + e] == slot_of[x] + e;
+        return all;
+    };
+    for (int x = tid; x < TT * hd; x += 256) {
+        const int t = x / hd, j = x % hd, s = t + R - 1, slot = slot_of[s];
+        if (slot < 0) continue;
+        const int row = slot % a.page_rows;
+        T* to = pool_at(a.v_pages, slot) + (row / R * hd + j) * R;
+        if (fills(s)) {
+            alignas(16) T unit[R];
+#pragma unroll
+            for (int e = 0; e < R; ++e) unit[e] = tile[(t + e) * hd + j];
+            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(unit);
+        } else if (!fills(s - slot % R)) {
+            to[row % R] = tile[t * hd + j];
+        }
+    }
+}
+
+// ---------------- missing-state fill on pages ----------------
+// A thread has one piece of a row (16 bytes of the key, or one element of the value) of one (token, KV head), reads it once from the source block
+// and writes it into a few of the dropped ones (grid.y).
+template <typename T>
+__global__ __launch_bounds__(256) void pages_fill_kernel(PagesFillArgs a, int layers_each) {
+    constexpr int R = 16 / sizeof(T);
+    const int k_pieces = a.hd / R, pieces = k_pieces + a.hd;
+    const long long x = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int piece = (int)(x % pieces), head = (int)(x / pieces % a.H_kv);
+    const long long t = x / pieces / a.H_kv;
+    if (t >= a.n) return;
+    const int slot = a.slots[t];
+    if (slot < 0 || slot >= a.n_slots) return;
+    const int row = slot % a.page_rows;
+    const size_t base = ((size_t)(slot / a.page_rows) * a.H_kv + head) * a.page_rows * a.hd;
+    const int l0 = a.first + blockIdx.y * layers_each, l1 = min(l0 + layers_each, a.first + a.n_layers);
+    if (piece < k_pieces) {
+        char* at = static_cast<char*>(a.k_pages) + (base + (size_t)row * a.hd + piece * R) * sizeof(T);
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (a.src >= 0) v = *reinterpret_cast<const uint4*>(at + a.src * a.pool_bytes);
+        for (int l = l0; l < l1; ++l) *reinterpret_cast<uint4*>(at + l * a.pool_bytes) = v;
+    } else {
+        char* at = static_cast<char*>(a.v_pages) + (base + (size_t)(row / R * a.hd + piece - k_pieces) * R + row % R) * sizeof(T);
+        T v{};
+        if (a.src >= 0) v = *reinterpret_cast<const T*>(at + a.src * a.pool_bytes);
+        for (int l = l0; l < l1; ++l) *reinterpret_cast<T*>(at + l * a.pool_bytes) = v;
+    }
+}
+
+template <typename T>
+int launch_append(const AppendArgs& a, hipStream_t s) {
+    const dim3 grid((a.n + kAppendTokens - 1) / kAppendTokens, a.H_kv, 2 * a.n_layers);
+    if (a.dtype == D3_F32) hipLaunchKernelGGL((pages_append_kernel<float, T>), grid, dim3(256), 0, s, a);
+    else if (a.dtype == D3_BF16) hipLaunchKernelGGL((pages_append_kernel<bf16_t, T>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((pages_append_kernel<f16_t, T>), grid, dim3(256), 0, s, a);
+    return (int)hipGetLastError();
+}
+
+}  // namespace
+
+int launch_pages_reserve(const ReserveArgs& a, hipStream_t s) {
+    // few tokens (a step's): by the same workgroup; many: by a launch of their own over the chip
+    const bool few = a.max_tokens <= 4 * kReserveThreads;
+    hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kReserveThreads), 0, s, a, few ? 1 : 0);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || few) return (int)e;
+    hipLaunchKernelGGL(pages_slots_kernel, dim3((unsigned)((a.max_tokens + 1023ll) / 1024)), dim3(256), 0, s, a);
+    return (int)hipGetLastError();
+}
+
+int launch_pages_append(const AppendArgs& a, int kv_dtype, hipStream_t s) {
+    return kv_dtype == D3_F32 ? launch_append<float>(a, s) : launch_append<f16_t>(a, s);
+}
+
+int launch_pages_fill(const PagesFillArgs& a, int kv_dtype, hipStream_t s) {
+    const long long threads = (long long)a.n * a.H_kv * (a.hd / unit_rows(kv_dtype) + a.hd);
+    const int each = 8;
+    const dim3 grid((unsigned)((threads + 255) / 256), (a.n_layers + each - 1) / each);
+    if (kv_dtype == D3_F32) hipLaunchKernelGGL(pages_fill_kernel<float>, grid, dim3(256), 0, s, a, each);
+    else hipLaunchKernelGGL(pages_fill_kernel<f16_t>, grid, dim3(256), 0, s, a, each);
+    return (int)hipGetLastError();
+}
+
+}  // namespace d3

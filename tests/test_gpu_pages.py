@@ -1,0 +1,569 @@
+"""The operators on a paged key-value cache against plain implementations in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+HALF_MAX = 65504.0
+
+
+def _types():
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def _cache(lens, heads, group, hd, kv, page_rows, layers=1, spare=3, seed=0, max_pages=None, room=0, fill="normal"):
+    """A cache whose sequences have the given rows on pages in random order, pools of random values (fill "nan": NaN wherever no sequence has a row)."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    held = [-(-(n + room) // page_rows) for n in lens]
+    cache = PagedCache(heads * group, heads, hd, sum(held) + spare, page_rows, len(lens), max_pages or max(max(held), 1), kv_dtype=kv, n_layers=layers, device=DEV)
+    order = torch.randperm(cache.n_pages, generator=g, device=DEV).int()
+    at = 0
+    for b, n in enumerate(held):
+        cache.tables[b, :n] = order[at: at + n]
+        at += n
+    cache.rows.copy_(torch.tensor(lens, dtype=torch.int32))
+    cache.k_pages.normal_(generator=g)
+    cache.v_pages.normal_(generator=g)
+    if fill == "nan":
+        for pool in (cache.k_pages, cache.v_pages):
+            mask = torch.ones(cache.n_pages * page_rows, dtype=torch.bool, device=DEV)
+            for b, n in enumerate(lens):
+                mask[_slots(cache, b, range(n))] = False
+            rows = _as_rows(cache, pool)
+            rows[:, mask] = math.nan
+            _from_rows(cache, pool, rows)
+    return cache, g
+
+
+def _slots(cache, b, rows):
+    import torch
+    p = torch.as_tensor(list(rows), dtype=torch.long, device=DEV)
+    return cache.tables[b].long()[p // cache.page_rows] * cache.page_rows + p % cache.page_rows
+
+
+def _as_rows(cache, pool):
+    """A pool as [layer][slot][head][dim] (a copy)."""
+    if pool is cache.v_pages:
+        L, n, h, blocks, hd, R = pool.shape
+        return pool.permute(0, 1, 3, 5, 2, 4).reshape(L, n * blocks * R, h, hd).clone()
+    L, n, h, pr, hd = pool.shape
+    return pool.permute(0, 1, 3, 2, 4).reshape(L, n * pr, h, hd).clone()
+
+
+def _from_rows(cache, pool, rows):
+    L, n = pool.shape[:2]
+    if pool is cache.v_pages:
+        _, _, h, blocks, hd, R = pool.shape
+        pool.copy_(rows.view(L, n, blocks, R, h, hd).permute(0, 1, 4, 2, 5, 3))
+    else:
+        _, _, h, pr, hd = pool.shape
+        pool.copy_(rows.view(L, n, pr, h, hd).permute(0, 1, 3, 2, 4))
+
+
+def _angles(positions, hd):
+    import torch
+    p = torch.as_tensor(positions, dtype=torch.float64, device=DEV)
+    a = p[:, None] * 10000.0 ** (-2.0 * torch.arange(hd // 2, dtype=torch.float64, device=DEV) / hd)
+    return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+
+
+def _turned(x, cs):
+    import torch
+    half = x.shape[-1] // 2
+    c, s = cs.double()[:, None, :, 0], cs.double()[:, None, :, 1]
+    a, b = x[..., :half], x[..., half:]
+    return torch.cat([a * c - b * s, a * s + b * c], -1)
+
+
+def _reference(cache, q, lens, layer=0, scale=None, gone=()):
+    """(out, allowed error) in 64 bits from the pools' values; `gone`: (sequence, page index) whose rows do not count.
+
+    The error: a score has the roundings of q (rotation: 3 of 2^-24; as two fp16 halves 2^-22), of 128 or fewer products summed in fp32 (hd of 2^-24) and of its own scaling
+    (2 of 2^-24), all relative to sum |q k|; that moves a weight by as much again as the maximum's score moves.  A weight has 2^-22 of its own (two halves, the exponential
+    and rescalings), and the sums over n rows n / 8 + 64 roundings at most in a row (32 or 16 rows a matrix instruction that adds 4 or 8 at a time; merges)."""
+    import torch
+    B, H, hd = q.shape
+    group = H // cache.n_kv_heads
+    scale = 1 / math.sqrt(hd) if scale is None else scale
+    K, V = (_as_rows(cache, p)[layer] for p in (cache.k_pages, cache.v_pages))
+    out, most = torch.zeros(B, H, hd, dtype=torch.float64, device=DEV), torch.zeros(B, H, 1, dtype=torch.float64, device=DEV)
+    for b, n in enumerate(lens):
+        rows = [j for j in range(n) if (b, j // cache.page_rows) not in gone]
+        if not rows:
+            continue
+        at = _slots(cache, b, rows)
+        k, v = K[at].double().repeat_interleave(group, 1), V[at].double().repeat_interleave(group, 1)
+        s = torch.einsum("hd,nhd->hn", q[b], k) * scale
+        out[b] = torch.einsum("hn,nhd->hd", torch.softmax(s, -1), v)
+        size = torch.einsum("hd,nhd->hn", q[b].abs(), k.abs()).amax(-1) * abs(scale)
+        each = 2.0 ** -22 + (hd + 5) * 2.0 ** -24
+        most[b, :, 0] = v.abs().amax((0, 2)) * (2 * each * size + 2.0 ** -21 + (n / 8 + 64) * 2.0 ** -24)
+    return out, most
+
+
+def _check(got, want, most):
+    import torch
+    step = torch.finfo(got.dtype).eps / 2
+    bad = (got.double() - want).abs() > most * 1.01 + step * want.abs() + 1e-30
+    assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, worst {float((got.double() - want).abs().max()):.3e}, allowed {float(most.max()):.3e}"
+
+
+EDGES = [0, 1, 2, 7, 8, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000]
+CASES = [  # lens, heads, group, hd, kv, act, page_rows, new rows, rotated
+    (EDGES, 2, 1, 128, "f16", "f32", 16, False, False),
+    (EDGES, 2, 2, 64, "f16", "bf16", 16, True, True),
+    (EDGES, 2, 4, 128, "f32", "f32", 16, True, True),
+    (EDGES, 1, 8, 64, "f32", "f16", 32, True, False),
+    (EDGES, 3, 3, 128, "f16", "f16", 64, False, True),
+    (EDGES, 1, 16, 128, "f16", "bf16", 128, True, True),
+    (EDGES, 1, 17, 128, "f16", "f32", 16, True, True),
+    ([300, 0, 77], 2, 40, 64, "f16", "f32", 32, True, True),
+    ([300, 1, 77], 1, 33, 128, "f32", "bf16", 16, True, True),
+    ([640], 32, 1, 128, "f16", "f32", 16, True, True),
+    ([1], 4, 1, 64, "f32", "f32", 16, True, True),
+    ([0, 0, 0], 4, 2, 128, "f16", "f32", 16, True, True),
+    ([20000], 1, 4, 128, "f16", "f32", 16, True, True),
+    ([9000, 3, 0, 4001], 2, 5, 64, "f32", "f32", 1024, True, True),
+    ([(37 * b) % 91 if b % 5 else 0 for b in range(200)], 2, 2, 128, "f16", "f32", 16, True, True),
+    ([0] * 130 + [5] + [0] * 69 + [700], 2, 1, 64, "f16", "f16", 16, True, False),
+]
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_attention_against_64_bits(case):
+    import torch
+    lens, heads, group, hd, kv, act, page_rows, new, rope = CASES[case]
+    cache, g = _cache(lens, heads, group, hd, kv, page_rows, seed=case, fill="nan")
+    B, H, t = len(lens), heads * group, _types()[act]
+    q = torch.empty(B, H, hd, dtype=t, device=DEV).normal_(generator=g)
+    k, v = (torch.empty(B, heads, hd, dtype=t, device=DEV).normal_(generator=g) for _ in range(2))
+    cs = _angles([max(n - 1, 0) for n in lens], hd) if rope else None
+    before = [_as_rows(cache, p) for p in (cache.k_pages, cache.v_pages)]
+    out = cache.attend(0, q, k if new else None, v if new else None, rope_cs=cs)
+    after = [_as_rows(cache, p) for p in (cache.k_pages, cache.v_pages)]
+    live = [b for b, n in enumerate(lens) if n > 0] if new else []
+    at = torch.cat([_slots(cache, b, [lens[b] - 1]) for b in live]) if live else torch.zeros(0, dtype=torch.long, device=DEV)
+    for was, now, x in zip(before, after, (_turned(k.double(), cs) if rope else k.double(), v.double())):
+        rest = torch.ones(was.shape[1], dtype=torch.bool, device=DEV)
+        rest[at] = False
+        assert torch.equal(was[:, rest].view(torch.uint8), now[:, rest].view(torch.uint8))
+        if not live:
+            continue
+        err = (now[0, at].double() - x[live]).abs()
+        # half a step of the cache's type, and the rotation's three roundings of 2^-24 relative to the two elements
+        assert (err <= torch.finfo(now.dtype).eps / 2 * x[live].abs() + 3 * 2.0 ** -24 * x[live].abs().amax() * 2 + 2.0 ** -25).all()
+    q64 = _turned(q.double(), cs) if rope else q.double()
+    _check(out, *_reference(cache, q64, lens))
+    assert torch.equal(out, cache.attend(0, q, k if new else None, v if new else None, rope_cs=cs))       # the same bits again
+
+
+def test_attention_scale_layers_strides_and_an_output_with_gaps():
+    import torch
+    heads, group, hd, lens = 2, 2, 128, [40, 300, 0, 9]
+    cache, g = _cache(lens, heads, group, hd, "f16", 16, layers=3, seed=5)
+    H = heads * group
+    buf = torch.empty(4, (H + 2 * heads) * hd + 32, device=DEV).normal_(generator=g)          # a projection's rows: q, k, v and something else
+    q, k, v = buf[:, : H * hd].view(4, H, hd), buf[:, H * hd: (H + heads) * hd].view(4, heads, hd), buf[:, (H + heads) * hd: (H + 2 * heads) * hd].view(4, heads, hd)
+    wide = torch.full((4, H * hd + 3), 7.0, device=DEV)
+    before = [p.clone() for p in (cache.k_pages, cache.v_pages)]
+    got = cache.attend(1, q, k, v, scale=-0.3, out=wide[:, 1: 1 + H * hd].view(4, H, hd))
+    _check(got, *_reference(cache, q.double(), lens, layer=1, scale=-0.3))
+    assert (wide[:, 0] == 7).all() and (wide[:, 1 + H * hd:] == 7).all()
+    for was, now in zip(before, (cache.k_pages, cache.v_pages)):
+        assert torch.equal(was[0], now[0]) and torch.equal(was[2], now[2]) and not torch.equal(was[1], now[1])
+
+
+def test_attention_leaves_out_pages_that_are_none():
+    import torch
+    lens, gone = [100, 33, 16, 64], {(0, 1), (0, 6), (1, 2), (2, 0), (3, 0), (3, 1)}
+    for kv in ("f16", "f32"):
+        cache, g = _cache(lens, 2, 4, 128, kv, 16, seed=6, spare=1)
+        spare = (set(range(cache.n_pages)) - set(cache.tables[cache.tables >= 0].tolist())).pop()
+        cache.k_pages[:, spare] = cache.v_pages[:, spare] = math.nan
+        good = cache.tables.clone()
+        for bad in (-1, cache.n_pages, 2 ** 31 - 1, -2 ** 31):
+            for b, j in gone:
+                cache.tables[b, j] = bad
+            q = torch.empty(4, 8, 128, device=DEV).normal_(generator=g)
+            k, v = (torch.empty(4, 2, 128, device=DEV).normal_(generator=g) for _ in range(2))
+            before = [p.clone() for p in (cache.k_pages, cache.v_pages)]
+            out = cache.attend(0, q, k, v)
+            cache.tables.copy_(good)
+            _check(out, *_reference(cache, q.double(), lens, gone=gone))
+            assert (out[2] == 0).all()
+            for was, now in zip(before, (cache.k_pages, cache.v_pages)):       # sequence 1's and 2's newest rows have no page, 0's has none either
+                changed = (was != now) & ~(was.isnan() & now.isnan())
+                assert set(changed.nonzero()[:, 1].tolist()) == {int(good[3, 3])}
+
+
+def test_attention_rows_past_the_table_are_cut_and_negative_ones_are_none():
+    import torch
+    cache, g = _cache([32, 16, 32], 2, 1, 64, "f16", 16, seed=7)
+    q = torch.empty(3, 2, 64, device=DEV).normal_(generator=g)
+    cache.rows.copy_(torch.tensor([10 ** 9, -5, 32], dtype=torch.int32))
+    _check(cache.attend(0, q), *_reference(cache, q.double(), [32, 0, 32]))
+
+
+def test_attention_of_infinities_and_nan_stays_with_its_sequence_and_heads():
+    import torch
+    for kv in ("f16", "f32"):
+        cache, g = _cache([50, 50, 50], 2, 2, 128, kv, 16, seed=8)
+        q = torch.empty(3, 4, 128, device=DEV).normal_(generator=g)
+        clean = cache.attend(0, q)
+        rows = _as_rows(cache, cache.v_pages)
+        rows[0, _slots(cache, 1, [20]), 1, 5] = math.nan
+        _from_rows(cache, cache.v_pages, rows)
+        out = cache.attend(0, q)
+        assert out[1, 2:, 5].isnan().all()
+        out[1, 2:, 5] = clean[1, 2:, 5]
+        assert torch.equal(out, clean)
+        q[2, 3] = math.nan
+        out = cache.attend(0, q)
+        assert out[2, 3].isnan().all() and torch.equal(out[2, :3], clean[2, :3]) and torch.equal(out[0], clean[0])
+
+
+def test_attention_large_scores_and_values():
+    """One row ahead of all others by more than fp32 exponents reach, and queries far from one."""
+    import torch
+    for kv in ("f16", "f32"):
+        cache, g = _cache([70, 300], 1, 2, 64, kv, 16, seed=9)
+        for size in (1e-6, 1e4):
+            q = torch.empty(2, 2, 64, device=DEV).normal_(generator=g) * size
+            out = cache.attend(0, q)
+            want, most = _reference(cache, q.double(), [70, 300])
+            if size > 1:                            # scores thousands apart: the weights are 0 and 1 wherever no two scores are within the error
+                s = torch.einsum("bhd,nhd->bhn", q.double(), _as_rows(cache, cache.k_pages)[0].double().repeat_interleave(2, 1)) / 8
+                assert out.isfinite().all() and float(s.abs().max()) > 1e4
+                same = (out.double() - want).abs() <= 1e-5 * want.abs() + 1e-6
+                assert same.double().mean() > 0.9
+            else:
+                _check(out, want, most)
+
+
+def test_attention_offsets_past_32_bits():
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    # 9000 pages of 2 heads x 1024 rows x 128: 4.7 GB a pool, 2.4e9 elements; the rows used are in the last pages
+    cache = PagedCache(4, 2, 128, 9000, 1024, 2, 2, device=DEV)
+    cache.tables.copy_(torch.tensor([[8999, 8997], [8998, -1]], dtype=torch.int32))
+    lens = [1500, 800]
+    cache.rows.copy_(torch.tensor(lens, dtype=torch.int32))
+    slots = torch.cat([_slots(cache, b, range(n)) for b, n in enumerate(lens)]).int()
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    k, v = (torch.empty(2300, 2, 128, device=DEV).normal_(generator=g) for _ in range(2))
+    cache.append(0, slots, k, v)
+    q = torch.empty(2, 4, 128, device=DEV).normal_(generator=g)
+    out = cache.attend(0, q)
+    for b, (lo, hi) in enumerate(((0, 1500), (1500, 2300))):
+        kk, vv = (x[lo:hi].half().double().repeat_interleave(2, 1) for x in (k, v))
+        s = torch.einsum("hd,nhd->hn", q[b].double(), kk) / math.sqrt(128)
+        want = torch.einsum("hn,nhd->hd", torch.softmax(s, -1), vv)
+        assert (out[b].double() - want).abs().max() < 1e-4
+    assert not cache.k_pages[0, :8997].any() and not cache.v_pages[0, :8997].any()
+
+
+APPENDS = [  # tokens, heads, hd, src, kv, page_rows, layers, rotated
+    (1, 1, 64, "f32", "f16", 16, 1, True), (77, 8, 64, "bf16", "f16", 16, 1, True), (64, 2, 128, "f16", "f32", 16, 2, False),
+    (65, 5, 128, "f32", "f32", 64, 1, True), (200, 2, 128, "f32", "f16", 128, 3, False), (130, 1, 128, "bf16", "f32", 32, 1, False), (300, 3, 64, "f16", "f16", 16, 1, True)]
+
+
+@pytest.mark.parametrize("case", range(len(APPENDS)))
+@pytest.mark.parametrize("order", ["run", "late", "runs", "mixed", "none"])
+def test_append_against_plain_indexing(case, order):
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    n, heads, hd, src, kv, page_rows, layers, rope = APPENDS[case]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(case)
+    n_pages = (n + 30) // page_rows + 4
+    cache = PagedCache(heads, heads, hd, n_pages, page_rows, 1, 1, kv_dtype=kv, n_layers=layers + 1, device=DEV)
+    cache.k_pages.normal_(generator=g)
+    cache.v_pages.normal_(generator=g)
+    total = n_pages * page_rows
+    pages = torch.randperm(n_pages, generator=g, device=DEV)
+    p = {"run": torch.arange(n), "late": torch.arange(5, n + 5), "runs": torch.arange(n) + torch.arange(n) // 23 * 3 % 19, "mixed": torch.arange(n), "none": torch.arange(n)}[order].to(DEV)
+    slots = pages[p // page_rows] * page_rows + p % page_rows
+    if order == "runs":                                    # pieces of 23 rows, each beginning where it likes
+        slots = torch.cat([torch.arange(23, device=DEV) + 26 * j for j in range(n // 23 + 1)])[:n] % total if n <= total - 30 else slots
+        slots = slots if slots.unique().numel() == n else pages[torch.arange(n, device=DEV) // page_rows] * page_rows + torch.arange(n, device=DEV) % page_rows
+    if order == "mixed":
+        slots = torch.randperm(total, generator=g, device=DEV)[:n]
+    slots = slots.int()
+    if order in ("none", "runs"):                          # some rows go nowhere
+        slots[::7] = torch.tensor([-1, total, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device=DEV).repeat(n)[: slots[::7].numel()]
+    t = _types()[src]
+    k, v = (torch.empty(layers, n, heads, hd, dtype=t, device=DEV).normal_(generator=g) for _ in range(2))
+    k[0, 0, 0, 0], v[0, 0, 0, 1] = 6e4 if src == "f16" else 1e5, -6e4 if src == "f16" else -1e5
+    cs = _angles(list(range(3, n + 3)), hd) if rope else None
+    before = [_as_rows(cache, x) for x in (cache.k_pages, cache.v_pages)]
+    cache.append(1, slots, k, v, rope_cs=cs)
+    live = ((slots >= 0) & (slots < total)).nonzero()[:, 0]
+    at = slots[live].long()
+    for was, pool, x in zip(before, (cache.k_pages, cache.v_pages), (_turned(k.double(), cs) if rope else k.double(), v.double())):
+        now, kept = _as_rows(cache, pool), torch.ones(total, dtype=torch.bool, device=DEV)
+        kept[at] = False
+        assert torch.equal(was[0], now[0]) and torch.equal(was[:, kept], now[:, kept])
+        x = x[:, live]
+        x = x.clamp(-HALF_MAX, HALF_MAX) if kv == "f16" else x
+        if not rope or pool is cache.v_pages:
+            assert torch.equal(now[1:, at], x.to(pool.dtype))          # rounded once, to nearest even
+        else:                                              # three roundings of 2^-24 relative to the pair, then half a step of the pool's type
+            half = hd // 2
+            pair = torch.maximum(k.double()[:, live].abs()[..., :half], k.double()[:, live].abs()[..., half:]).repeat(1, 1, 1, 2)
+            assert ((now[1:, at].double() - x).abs() <= torch.finfo(pool.dtype).eps / 2 * x.abs() + 6 * 2.0 ** -24 * pair + 2.0 ** -25).all()
+
+
+def test_append_strides_nan_and_no_rows():
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    cache = PagedCache(2, 2, 64, 4, 16, 1, 1, device=DEV)
+    buf = torch.randn(20, 2, 2, 3, 64, device=DEV)          # token, head, other things
+    k, v = buf[:, :, 0, 0], buf[:, :, 1, 2]
+    v[3, 1, 7], k[4, 0, 9] = math.nan, math.inf
+    slots = torch.arange(7, 27, dtype=torch.int32, device=DEV)
+    cache.append(0, slots, k, v)
+    K, V = (_as_rows(cache, x)[0] for x in (cache.k_pages, cache.v_pages))
+    assert torch.equal(K[7:27], k.clamp(-HALF_MAX, HALF_MAX).half())
+    assert V[10, 1, 7].isnan() and int(V.isnan().sum()) == 1 and torch.equal(torch.nan_to_num(V[7:27]), torch.nan_to_num(v.half()))
+    assert not K[:7].any() and not K[27:].any()
+    cache.append(0, slots[:0], k[:0], v[:0])
+
+
+@pytest.mark.parametrize("kv,heads,hd,page_rows", [("f16", 3, 128, 16), ("f32", 2, 64, 32), ("f16", 1, 64, 16)])
+def test_fill_copies_rows_into_the_dropped_layers(kv, heads, hd, page_rows):
+    import torch
+    cache, g = _cache([40, 33], heads, 1, hd, kv, page_rows, layers=20, seed=3)
+    slots = torch.cat([_slots(cache, 0, [39, 0, 17]), _slots(cache, 1, [32])]).int()
+    slots = torch.cat([slots, slots[:1], torch.tensor([-1, cache.n_pages * page_rows], dtype=torch.int32, device=DEV)])      # one row twice, two that are none
+    for src, first, n in ((4, 5, 15), (19, 0, 3), (7, 8, 1), (-1, 2, 9)):
+        before = [_as_rows(cache, x) for x in (cache.k_pages, cache.v_pages)]
+        cache.fill(slots, src, first, n)
+        at = slots[:4].long()
+        for was, pool in zip(before, (cache.k_pages, cache.v_pages)):
+            want = was.clone()
+            for l in range(first, first + n):
+                want[l, at] = was[src, at] if src >= 0 else 0
+            assert torch.equal(_as_rows(cache, pool), want)
+    cache.fill(slots[:0], 0, 1, 1)
+    cache.fill(slots, 0, 1, 0)
+
+
+# ---------------- page tables and slot maps ----------------
+
+def _reserve_plainly(rows, added, tables, stack, page_rows, max_pages, max_tokens):
+    rows, tables, stack = list(rows), [list(t) for t in tables], list(stack)
+    for b, a in enumerate(added):
+        if a < 0:
+            stack += tables[b][: -(-rows[b] // page_rows)]
+            rows[b] = 0
+    avail, asked, pages, starts, slots, positions = len(stack), 0, 0, [0], [], []
+    for b, a in enumerate(added):
+        if a > 0 and rows[b] + a <= max_pages * page_rows:
+            asked += a
+            if asked <= max_tokens:
+                first, end = -(-rows[b] // page_rows), -(-(rows[b] + a) // page_rows)
+                pages += end - first
+                if first == end or pages <= avail:
+                    for j in range(first, end):
+                        tables[b][j] = stack.pop()
+                    for p in range(rows[b], rows[b] + a):
+                        slots.append(tables[b][p // page_rows] * page_rows + p % page_rows)
+                        positions.append(p)
+                    rows[b] += a
+        starts.append(len(slots))
+    none = [-1] * (max_tokens - len(slots))
+    return rows, tables, stack, max(0, pages - avail), starts, slots + none, positions + none
+
+
+@pytest.mark.parametrize("B,page_rows,max_pages,n_pages,longest,max_tokens", [
+    (1, 16, 4, 3, 40, 50), (5, 16, 8, 20, 60, 100), (7, 32, 3, 40, 100, 90), (64, 16, 10, 300, 40, 900), (65, 16, 10, 200, 40, 5000), (333, 64, 4, 700, 200, 20000),
+    (1025, 16, 3, 1500, 30, 9000), (4096, 16, 2, 5000, 20, 30000), (3, 1024, 2, 5, 1500, 0)])
+def test_reserve_over_many_steps_against_a_plain_list(B, page_rows, max_pages, n_pages, longest, max_tokens):
+    """Requests that come, grow and end, more than there is room for; the stack, tables and maps after every call."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    cache = PagedCache(1, 1, 64, n_pages, page_rows, B, max_pages, device=DEV)
+    rng = np.random.RandomState(B)
+    rows, tables, stack = [0] * B, cache.tables.tolist(), list(range(n_pages - 1, -1, -1))
+    granted = refused = 0
+    for step in range(12):
+        kind = rng.randint(0, 6, B)
+        added = np.where(kind == 0, -rng.randint(1, 5, B), np.where(kind == 1, 0, np.where(kind == 2, rng.randint(1, longest, B), 1)))
+        if step == 3:
+            added[:] = -1
+        if step == 7:
+            added[rng.randint(B)] = 2 ** 31 - 1
+        want = _reserve_plainly(rows, added.tolist(), tables, stack, page_rows, max_pages, max_tokens)
+        added_t = torch.tensor(added, dtype=torch.int32, device=DEV)
+        if step % 3 == 1:                                  # asked without taking, then taken: the same answer, and the state as it was in between
+            rows_out, n_free_out = torch.empty_like(cache.rows), torch.empty_like(cache.n_free)
+            was = cache.rows.clone(), cache.n_free.clone()
+            first = [x.clone() for x in cache.reserve(added_t, max_tokens, rows_out=rows_out, n_free_out=n_free_out)]
+            assert torch.equal(was[0], cache.rows) and torch.equal(was[1], cache.n_free) and rows_out.tolist() == want[0] and n_free_out.tolist() == [len(want[2]), want[3]]
+        starts, slots, positions = cache.reserve(added_t, max_tokens)
+        if step % 3 == 1:
+            assert all(torch.equal(x, y) for x, y in zip(first, (starts, slots, positions)))
+        rows, tables, stack = want[:3]
+        assert cache.rows.tolist() == rows and cache.tables.tolist() == tables
+        assert cache.n_free.tolist() == [len(stack), want[3]] and cache.free_pages[: len(stack)].tolist() == stack
+        assert starts.tolist() == want[4] and slots.tolist() == want[5] and positions.tolist() == want[6]
+        granted += starts[-1].item()
+        refused += int((added > 0).sum()) - int((np.diff(want[4]) > 0).sum())
+    assert refused > 0 and (granted > 0 or max_tokens == 0)
+
+
+def test_reserve_bounds_a_state_that_is_wrong():
+    """Rows and counts outside their ranges, and page numbers that are none: everything stays inside its buffers, tokens without a page get no slot."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    cache = PagedCache(1, 1, 64, 6, 16, 4, 3, device=DEV)
+    cache.rows.copy_(torch.tensor([-7, 10 ** 6, 16, 2], dtype=torch.int32))
+    cache.n_free.copy_(torch.tensor([10 ** 6, 0], dtype=torch.int32))
+    cache.free_pages[:] = torch.tensor([5, 4, 99, -3, 1, 0], dtype=torch.int32)
+    starts, slots, positions = cache.reserve(torch.tensor([33, 1, 20, -1], dtype=torch.int32, device=DEV), 80)
+    assert starts.tolist() == [0, 33, 33, 53, 53]           # the second is full; the fourth's page has no place on a full stack
+    # pages popped: sequence 0: 0, 1, -3; sequence 2: 99, 4
+    assert cache.tables.tolist() == [[0, 1, -3], [-1, -1, -1], [-1, 99, 4], [-1, -1, -1]]
+    want = list(range(16)) + list(range(16, 32)) + [-1] + [-1] * 16 + list(range(64, 68)) + [-1] * 27
+    assert slots.tolist() == want and positions[:53].tolist() == list(range(33)) + list(range(16, 36))
+    assert cache.rows.tolist() == [33, 48, 36, 0] and cache.n_free.tolist() == [1, 0]
+
+
+# ---------------- used together ----------------
+
+def test_operators_together_as_a_server_uses_them():
+    """Requests of unequal length come in, decode, end and make room: reserve, append, attend and fill on two layers, against lists of rows in 64 bits."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    heads, group, hd, B, layers = 2, 4, 64, 5, 3
+    for kv in ("f16", "f32"):
+        cache = PagedCache(heads * group, heads, hd, 14, 16, B, 6, kv_dtype=kv, n_layers=layers, device=DEV)
+        g = torch.Generator(device=DEV)
+        g.manual_seed(2)
+        normal = lambda *dims: torch.empty(dims, device=DEV).normal_(generator=g)
+        K, V = ([[torch.zeros(0, heads, hd, dtype=torch.float64, device=DEV) for _ in range(B)] for _ in range(layers)] for _ in range(2))
+        steps = [[17, 40, 0, 0, 3], [1, 1, 70, 0, 1], [1, -1, 1, 20, 1], [1, 30, 1, 1, 1], [-1, 1, -1, 1, 1], [60, 1, 0, 1, 1], [1, 1, 9, 1, 1]]
+        for added in steps:
+            added_t = torch.tensor(added, dtype=torch.int32, device=DEV)
+            starts, slots, positions = cache.reserve(added_t, 100)
+            n = np.diff(starts.tolist())
+            for l in range(layers):
+                for b in range(B):
+                    if added[b] < 0:
+                        K[l][b], V[l][b] = K[l][b][:0], V[l][b][:0]
+            total = int(n.sum())
+            cs = _angles(positions[:total].tolist(), hd)
+            for l in range(layers - 1):                    # the last layer is dropped in every step and filled
+                k, v = normal(100, heads, hd), normal(100, heads, hd)
+                cs_all = torch.zeros(100, hd // 2, 2, device=DEV)
+                cs_all[:total] = cs
+                cache.append(l, slots, k, v, rope_cs=cs_all)
+                r = _turned(k[:total].double(), cs)
+                for b in range(B):
+                    at = slice(int(starts[b]), int(starts[b + 1]))
+                    K[l][b], V[l][b] = torch.cat([K[l][b], r[at]]), torch.cat([V[l][b], v[at].double()])
+            cache.fill(slots, layers - 2, layers - 1, 1)
+            K[-1], V[-1] = list(K[-2]), list(V[-2])
+            assert cache.rows.tolist() == [x.shape[0] for x in K[0]]
+            for l in range(layers):
+                q = normal(B, heads * group, hd)
+                out = cache.attend(l, q)
+                for b in range(B):
+                    if not len(K[l][b]):
+                        assert not out[b].any()
+                        continue
+                    s = torch.einsum("hd,nhd->hn", q[b].double(), K[l][b].repeat_interleave(group, 1)) / math.sqrt(hd)
+                    want = torch.einsum("hn,nhd->hd", torch.softmax(s, -1), V[l][b].repeat_interleave(group, 1))
+                    # rows are held to half a step: 2^-11 (or 2^-24) of |q||k| in a score, twice that in a weight, and of a value
+                    eps = 2.0 ** -11 if kv == "f16" else 2.0 ** -22
+                    size = torch.einsum("hd,nhd->hn", q[b].double().abs(), K[l][b].abs().repeat_interleave(group, 1)).max() / math.sqrt(hd)
+                    assert (out[b].double() - want).abs().max() <= (2 * size + 1) * eps * V[l][b].abs().max() + 1e-4
+
+
+def test_a_captured_step_replayed_while_sequences_grow():
+    """reserve and attend captured once; every replay is checked against eager calls on a second cache."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    heads, group, hd, B = 4, 2, 128, 3
+    caches = [PagedCache(heads * group, heads, hd, 60, 16, B, 20, device=DEV) for _ in range(2)]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(4)
+    first = torch.tensor([30, 1, 200], dtype=torch.int32, device=DEV)
+    k, v = (torch.empty(231, heads, hd, device=DEV).normal_(generator=g) for _ in range(2))
+    for c in caches:
+        _, slots, _ = c.reserve(first, 231)
+        c.append(0, slots, k, v)
+    ones = torch.ones(B, dtype=torch.int32, device=DEV)
+    q, nk, nv = torch.empty(B, heads * group, hd, device=DEV), torch.empty(B, heads, hd, device=DEV), torch.empty(B, heads, hd, device=DEV)
+    starts, slots, positions = (torch.empty(n, dtype=torch.int32, device=DEV) for n in (B + 1, B, B))
+    out = torch.empty_like(q)
+    torch.cuda.synchronize()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=stream):
+        caches[0].reserve(ones, B, starts=starts, slots=slots, positions=positions)
+        caches[0].attend(0, q, nk, nv, out=out)
+    for step in range(25):
+        for x in (q, nk, nv):
+            x.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        s2, m2, p2 = caches[1].reserve(ones, B)
+        want = caches[1].attend(0, q, nk, nv)
+        assert torch.equal(starts, s2) and torch.equal(slots, m2) and torch.equal(positions, p2)
+        assert torch.equal(out, want) and torch.equal(caches[0].rows, caches[1].rows)
+        assert torch.equal(caches[0].k_pages, caches[1].k_pages) and torch.equal(caches[0].v_pages, caches[1].v_pages)
+    assert caches[0].rows.tolist() == [55, 26, 225]
+
+
+def test_calls_on_another_stream():
+    import torch
+    cache, g = _cache([100, 5], 2, 2, 128, "f16", 16, seed=11, room=1)
+    q = torch.empty(2, 4, 128, device=DEV).normal_(generator=g)
+    want = cache.attend(0, q)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        got = cache.attend(0, q)
+    stream.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_refusals():
+    import torch
+    from paper_2503_08524_amd import D3Error, PagedCache
+    cache = PagedCache(4, 2, 64, 8, 16, 3, 4, n_layers=2, device=DEV)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    q, k = torch.zeros(3, 4, 64, device=DEV), torch.zeros(3, 2, 64, device=DEV)
+    slots = ints(0, 1, 2)
+    for call in (lambda: cache.reserve(ints(1, 1, 1, 1), 4), lambda: cache.reserve(torch.ones(3, device=DEV), 4), lambda: cache.reserve(ints(1), 4, slots=ints(0)),
+                 lambda: cache.reserve(ints(1), -1), lambda: cache.reserve(torch.ones(1, dtype=torch.int32), 1),
+                 lambda: cache.append(0, slots, k, k[:2]), lambda: cache.append(0, slots, k, k.half()), lambda: cache.append(0, slots.long(), k, k),
+                 lambda: cache.append(0, slots, k.double(), k.double()), lambda: cache.append(0, slots, k, k, rope_cs=torch.zeros(3, 64, device=DEV)),
+                 lambda: cache.attend(0, k), lambda: cache.attend(0, q, k), lambda: cache.attend(0, q, k.half(), k.half()), lambda: cache.attend(0, q, out=q.half()),
+                 lambda: cache.attend(0, q.transpose(1, 2).contiguous().transpose(1, 2)), lambda: cache.attend(0, q, rope_cs=torch.zeros(2, 32, 2, device=DEV)),
+                 lambda: cache.fill(slots.long(), 0, 1, 1), lambda: PagedCache(4, 2, 64, 8, 16, 3, 4, kv_dtype="f8"),
+                 lambda: PagedCache(4, 2, 64, 8, 16, 3, 4, rows=ints(0, 0)), lambda: PagedCache(4, 2, 64, 8, 16, 3, 4, k_pages=torch.zeros(1, 8, 2, 16, 64, device=DEV))):
+        with pytest.raises(ValueError):
+            call()
+    wide = torch.zeros(3 * 258 + 8, device=DEV)
+    for call, status, word in ((lambda: cache.append(2, slots, k, k), -3, "layers"), (lambda: cache.append(1, slots, k.expand(2, 3, 2, 64).contiguous(), k.expand(2, 3, 2, 64).contiguous()), -3, "layers"),
+                               (lambda: cache.append(-1, slots, k, k), -3, "layers"), (lambda: cache.attend(2, q), -3, "layers"),
+                               (lambda: cache.attend(0, torch.zeros(4, 4, 64, device=DEV)), -2, "B must be"), (lambda: cache.attend(0, q, scale=math.inf), -1, "scale"),
+                               (lambda: cache.attend(0, q, scale=math.nan), -1, "scale"),
+                               (lambda: cache.attend(0, wide[1: 769].view(3, 4, 64)), -1, "16 bytes"), (lambda: cache.attend(0, wide[:774].view(3, 258)[:, :256].view(3, 4, 64)), -1, "16 bytes"),
+                               (lambda: cache.append(0, slots, wide[1: 385].view(3, 2, 64), wide[1: 385].view(3, 2, 64)), -1, "16 bytes"),
+                               (lambda: cache.fill(slots, 1, 0, 2), -3, "source layer"), (lambda: cache.fill(slots, 2, 0, 1), -3, "source layer"),
+                               (lambda: cache.fill(slots, 0, 1, 2), -3, "layers"), (lambda: cache.reserve(ints(), 0), -1, "NULL"),
+                               (lambda: PagedCache(4, 3, 64, 8, 16, 3, 4), -2, "multiple"), (lambda: PagedCache(4, 2, 64, 8, 16, 3, 4, kv_dtype="bf16"), -2, "D3_BF16")):
+        with pytest.raises(D3Error) as e:
+            call()
+        assert e.value.status == status and word in str(e.value)
+    assert not cache.k_pages.any() and not cache.v_pages.any()
