@@ -42,12 +42,15 @@ struct PagedShape {
     static constexpr float SHIFT = ES == 2 ? 15.f : 0.f;
 };
 
-template <int HD>
+template <typename T, int HD>
 struct PagedShared {
-    float m[kPagedHeads][4], l[kPagedHeads][4];    // per wave: running max and sum of each head
     float o[4][kPagedHeads][HD + 4];               // per wave: unnormalised outputs (rows 4 words apart in the banks)
+    float m[kPagedHeads][4], l[kPagedHeads][4];    // per wave: running max and sum of each head
+    T new_k[HD], new_v[HD];                        // the newest row as the pool holds it
     int is_last;
 };
+
+constexpr int kJoin = 16;      // partial results that one workgroup joins at a time, all of their loads in flight together
 
 // N consecutive activations
 template <int N>
@@ -84,30 +87,51 @@ __device__ __forceinline__ float load_act1(const void* p, long long at, int dtyp
     const uint16_t h = static_cast<const uint16_t*>(p)[at];
     return dtype == D3_BF16 ? bf16_to_f32(h) : (float)__builtin_bit_cast(_Float16, h);
 }
-__device__ __forceinline__ void store_act(void* p, long long at, int dtype, float v) {
-    if (dtype == D3_F32) static_cast<float*>(p)[at] = v;
-    else if (dtype == D3_BF16) static_cast<uint16_t*>(p)[at] = (uint16_t)bf16_pair(v, 0.f);
-    else static_cast<_Float16*>(p)[at] = (_Float16)v;
-}
-
-__device__ __forceinline__ int scan_wave(int v) {                  // inclusive
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const int below = __shfl_up(v, o, 64);
-        if (lane >= o) v += below;
+// four consecutive ones; `whole`: they lie on a multiple of their size
+__device__ __forceinline__ void store_act4(void* p, long long at, int dtype, const float (&v)[4], bool whole) {
+    if (dtype == D3_F32) {
+        float* f = static_cast<float*>(p) + at;
+        if (whole) *reinterpret_cast<float4*>(f) = make_float4(v[0], v[1], v[2], v[3]);
+        else { f[0] = v[0]; f[1] = v[1]; f[2] = v[2]; f[3] = v[3]; }
+        return;
     }
-    return v;
+    uint2 w;
+    if (dtype == D3_BF16) w = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+    else {
+        typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+        w = __builtin_bit_cast(uint2, half4{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]});
+    }
+    uint16_t* h = static_cast<uint16_t*>(p) + at;
+    if (whole) *reinterpret_cast<uint2*>(h) = w;
+    else { h[0] = (uint16_t)w.x; h[1] = (uint16_t)(w.x >> 16); h[2] = (uint16_t)w.y; h[3] = (uint16_t)(w.y >> 16); }
 }
 
-// Equal runs of `total` chunks: the first `over` workgroups have one more.
+// st_agent, ld_agent of two adjacent floats
+__device__ __forceinline__ void st_agent2(float* p, float x, float y) {
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 ld_agent2(const float* p) {
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+
+__device__ __forceinline__ int scan_wave(int v) {                  // inclusive: within rows of 16 lanes, then over the rows
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+    return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+}
+
+// Equal runs of `total` units: the first `over` workgroups have one more.
 struct Runs {
     int per, over;
     __device__ Runs(int total, int n) : per((int)((unsigned)total / (unsigned)n)), over(total - per * n) {}
     __device__ int begin(int w) const { return w * per + min(w, over); }
-    __device__ int of(int x) const {                               // the run that chunk x is in
+    __device__ int of(int x) const {                               // the run that unit x is in
         const int larger = over * (per + 1);
-        return x < larger ? x / (per + 1) : over + (x - larger) / per;      // per = 0: every chunk is below `larger`
+        return x < larger ? x / (per + 1) : over + (x - larger) / per;      // per = 0: every unit is below `larger`
     }
 };
 
@@ -115,33 +139,37 @@ template <typename T, int HD>
 __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
     typedef PagedShape<T, HD> P;
     constexpr int R = P::R, KT = P::KT, RG = P::RG, NK = P::NK, ND = P::ND, U = P::U, QE = P::QE;
-    __shared__ PagedShared<HD> sh;
+    __shared__ PagedShared<T, HD> sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
     const int H = a.H_kv * a.group, tiles = (a.group + kPagedHeads - 1) / kPagedHeads, HH = a.H_kv * tiles, GP = min(a.group, kPagedHeads);
     auto length = [&](int b) { return min(max(a.rows[b], 0), a.max_rows); };
 
-    // ---- this workgroup's run of chunks, and where it begins ----
-    auto chunks_of = [&](int b) { return b < a.B ? (length(b) + P::CH - 1) / P::CH * HH : 0; };
-    int n = chunks_of(lane), upto = scan_wave(n), total = __builtin_amdgcn_readlane(upto, 63);
+    // ---- this workgroup's run of units, and where it begins ----
+    auto units_of = [&](int b) {
+        const int len = b < a.B ? length(b) : 0;
+        return len > 0 ? ((len + P::CH - 1) / P::CH + kPagedOverhead) * HH : 0;
+    };
+    int n = units_of(lane), upto = scan_wave(n), total = __builtin_amdgcn_readlane(upto, 63);
     const int total64 = total;
-    for (int b0 = 64; b0 < a.B; b0 += 64) total += __builtin_amdgcn_readlane(scan_wave(chunks_of(b0 + lane)), 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64) total += __builtin_amdgcn_readlane(scan_wave(units_of(b0 + lane)), 63);
     for (int b = blockIdx.x; b < a.B; b += gridDim.x) {             // a sequence without rows: zeros
         if (length(b) > 0) continue;
-        for (int e = tid; e < H * HD; e += 256) {
-            store_act(a.out, b * a.out_stride + e, a.dtype, 0.f);
-            if (a.out_split) store_split1(a.out_split + b * a.out_form.pitch(H * HD), e, 0.f, a.out_form.lo);
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int e = tid * 4; e < H * HD; e += 1024) {
+            store_act4(a.out, b * a.out_stride + e, a.dtype, zero, false);
+            if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H * HD), e, zero, a.out_form.lo);
         }
     }
     const Runs runs(total, gridDim.x);
     const int run = blockIdx.x, end = runs.begin(run + 1);
     int u = runs.begin(run);
     if (u >= end) return;
-    int b = 0, seq_begin = 0;                                       // the sequence of chunk u, and its first chunk
+    int b = 0, seq_begin = 0;                                       // the sequence of unit u, and its first unit
     {
         int before = 0, b0 = 0, here = total64;
         while (u >= before + here) {
             before += here; b0 += 64;
-            n = chunks_of(b0 + lane); upto = scan_wave(n); here = __builtin_amdgcn_readlane(upto, 63);
+            n = units_of(b0 + lane); upto = scan_wave(n); here = __builtin_amdgcn_readlane(upto, 63);
         }
         const int at = __builtin_ctzll(__ballot(before + upto > u));
         b = b0 + at;
@@ -150,13 +178,16 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 
     const int block_shift = a.page_shift - (R == 8 ? 3 : 2), block_mask = (1 << block_shift) - 1;      // blocks of R rows
     const size_t head_bytes = ((size_t)HD * P::ES) << a.page_shift, page_bytes = head_bytes * a.H_kv;
+    const bool out_whole = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_stride % 4 == 0;
 
     while (u < end) {
         const int len = __builtin_amdgcn_readfirstlane(length(b));
-        const int per_head = (len + P::CH - 1) / P::CH, hh = (u - seq_begin) / per_head, head_begin = seq_begin + hh * per_head;
-        const int c0 = u - head_begin, c1 = min(per_head, c0 + end - u);
+        const int chunks = (len + P::CH - 1) / P::CH, per_head = chunks + kPagedOverhead, hh = (u - seq_begin) / per_head, head_begin = seq_begin + hh * per_head;
+        const int c0 = max(u - head_begin - kPagedOverhead, 0), c1 = min(chunks, end - head_begin - kPagedOverhead);
+        const int next = min(end, head_begin + per_head);
+        if (c1 <= 0) return;                                        // the run ends in the overhead of this one
         const int kvh = hh / tiles, h0 = (hh - kvh * tiles) * kPagedHeads, nh = min(kPagedHeads, a.group - h0);
-        const bool whole = c0 == 0 && c1 == per_head;
+        const bool whole = c0 == 0 && c1 == chunks;
         const int newest = len - 1, last_block = newest / R;
         const int* tab = a.tables + (size_t)b * a.table_stride;
         char* Kh = static_cast<char*>(a.k_pages) + kvh * head_bytes;
@@ -209,11 +240,20 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             }
         };
 
+        // the wave whose turn has the newest row rounds it as the pool does, and puts it into its page
+        const bool fresh = a.k_new && c1 == chunks && (newest / P::TR & 3) == wave;
         float m = -INFINITY, l = 0.f;
         f32x4 acc[ND];
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (r < rend) {
+            float2 nk = {0.f, 0.f}, nv = {0.f, 0.f}, ncs = {1.f, 0.f};      // dims `lane` and lane + HD / 2 of the newest row
+            if (fresh && lane < HD / 2) {
+                const long long at = b * a.kv_stride + (long long)kvh * HD + lane;
+                nk = make_float2(load_act1(a.k_new, at, a.dtype), load_act1(a.k_new, at + HD / 2, a.dtype));
+                nv = make_float2(load_act1(a.v_new, at, a.dtype), load_act1(a.v_new, at + HD / 2, a.dtype));
+                if (a.rope_cs) ncs = a.rope_cs[(size_t)b * (HD / 2) + lane];
+            }
             int pk[U], pv[U], pk1[U], pv1[U];
             load_pages(r, pk, pv);
             load_pages(r + P::CH, pk1, pv1);
@@ -222,6 +262,23 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             for (int k = 0; k < NK; ++k) load_act<QE>(a.q, b * a.q_stride + (long long)(kvh * a.group + h0 + min(i, nh - 1)) * HD + k * 4 * QE + g * QE, a.dtype, qf[k]);
             issue_k(r, pk);
             issue_v(r, pv);
+            __builtin_amdgcn_sched_barrier(0);
+            if (fresh) {
+                const int page = tab[last_block >> block_shift];
+                if (lane < HD / 2) {
+                    const float y[2] = {nk.x * ncs.x - nk.y * ncs.y, nk.y * ncs.x + nk.x * ncs.y}, z[2] = {nv.x, nv.y};
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int d = lane + e * (HD / 2);
+                        const T kt = held<T>(y[e]), vt = held<T>(z[e]);
+                        sh.new_k[d] = kt; sh.new_v[d] = vt;
+                        if (h0 == 0 && present(page)) {
+                            reinterpret_cast<T*>(Kh + page * page_bytes)[(newest & ((1 << a.page_shift) - 1)) * HD + d] = kt;
+                            reinterpret_cast<T*>(Vh + page * page_bytes)[((last_block & block_mask) * HD + d) * R + newest % R] = vt;
+                        }
+                    }
+                }
+            }
             if (a.rope_cs) rotated(qf);
             // q as fp16 halves hi + lo, scaled by a power of two that puts its largest element at 2^14: 22 bits of it
             float mul = a.scale * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
@@ -252,33 +309,15 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 #pragma unroll
                 for (int x = 0; x < U; ++x) absent = absent || !present(pv[x]);
                 absent = __any(absent);
-                if (!MORE && tail && a.k_new) {                     // the newest row's key takes its place among the rows
-                    float y[NK][QE];
-#pragma unroll
-                    for (int k = 0; k < NK; ++k) load_act<QE>(a.k_new, b * a.kv_stride + (long long)kvh * HD + k * 4 * QE + g * QE, a.dtype, y[k]);
-                    if (a.rope_cs) rotated(y);
-                    uint4 nk[NK];
-#pragma unroll
-                    for (int k = 0; k < NK; ++k) {
-                        T h[QE];
-#pragma unroll
-                        for (int e = 0; e < QE; ++e) h[e] = held<T>(y[k][e]);
-                        __builtin_memcpy(&nk[k], h, 16);
-                    }
+                if (!MORE && fresh) {                               // the newest row's key takes its place among the rows
 #pragma unroll
                     for (int x = 0; x < U; ++x)
 #pragma unroll
                         for (int t = 0; t < KT; ++t) {
                             if (r + x * RG + R * (i >> 2) + 4 * t + (i & 3) != newest) continue;
 #pragma unroll
-                            for (int k = 0; k < NK; ++k) kr[x][t][k] = nk[k];
+                            for (int k = 0; k < NK; ++k) kr[x][t][k] = *reinterpret_cast<const uint4*>(&sh.new_k[k * 4 * QE + g * QE]);
                         }
-                    const int page = tab[last_block >> block_shift];
-                    if (h0 == 0 && i == 0 && newest >= r && present(page)) {       // and its place in the cache
-                        char* to = Kh + page * page_bytes + (newest & ((1 << a.page_shift) - 1)) * (HD * P::ES) + g * 16;
-#pragma unroll
-                        for (int k = 0; k < NK; ++k) *reinterpret_cast<uint4*>(to + k * 64) = nk[k];
-                    }
                 }
                 float s[U][R];
 #pragma unroll
@@ -349,17 +388,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                             T v[R];
                             __builtin_memcpy(v, &vr[x][d], 16);
                             T own{};
-                            if (!MORE && a.k_new && newest >= row0 && newest < row0 + R) own = held<T>(load_act1(a.v_new, b * a.kv_stride + (long long)kvh * HD + d * 16 + i, a.dtype));
+                            if (!MORE && fresh) own = sh.new_v[d * 16 + i];
 #pragma unroll
                             for (int e = 0; e < R; ++e) {
-                                if (!MORE && a.k_new && row0 + e == newest) v[e] = own;
+                                if (!MORE && fresh && row0 + e == newest) v[e] = own;
                                 if (!present(pv[x]) || row0 + e >= len) v[e] = (T)0.f;
                             }
                             __builtin_memcpy(&vr[x][d], v, 16);
-                            if (!MORE && a.k_new && h0 == 0 && newest >= row0 && newest < row0 + R && present(pv[x])) {
-                                char* to = Vh + pv[x] * page_bytes + (last_block & block_mask) * (HD * 16) + (d * 16 + i) * 16 + (newest - row0) * P::ES;
-                                *reinterpret_cast<T*>(to) = own;
-                            }
                         }
                     }
                 }
@@ -402,75 +437,111 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(&sh.o[wave][i][d * 16 + g * 4]) = acc[d];
         }
         __syncthreads();
-        auto finish = [&](int h, int t, float o, float sum) {
-            const float v = sum == 0.f ? 0.f : o / sum;             // no row counted: zeros
+        const int items = nh * (HD / 4);                            // a thread has four dims of a head
+        auto finish = [&](int h, int t, const float (&o)[4], float sum) {
+            const float by = sum == 0.f ? 0.f : 1.f / sum;          // no row counted: zeros
+            const float v[4] = {o[0] * by, o[1] * by, o[2] * by, o[3] * by};
             const int e = (kvh * a.group + h0 + h) * HD + t;
-            store_act(a.out, b * a.out_stride + e, a.dtype, v);
-            if (a.out_split) store_split1(a.out_split + b * a.out_form.pitch(H * HD), e, v, a.out_form.lo);
+            store_act4(a.out, b * a.out_stride + e, a.dtype, v, out_whole);
+            if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H * HD), e, v, a.out_form.lo);
         };
-        // this run's partials: a run has at most two, of the (sequence, heads) that it begins in and of the one that it ends in
-        const size_t slot = 2 * (size_t)run + (u == runs.begin(run) ? 0 : 1);
-        for (int idx = tid; idx < nh * HD; idx += 256) {
-            const int h = idx / HD, t = idx % HD;
+        auto publish = [&](size_t slot, int h, int t, const float (&o)[4], float M, float L) {
+            float* p = &a.part_o[(slot * GP + h) * HD + t];
+            st_agent2(p, o[0], o[1]);
+            st_agent2(p + 2, o[2], o[3]);
+            if (t == 0) st_agent2(&a.part_ml[(slot * GP + h) * 2], M, L);
+        };
+        // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
+        const int w0 = runs.of(head_begin + kPagedOverhead), w1 = runs.of(head_begin + per_head - 1), parts = w1 - w0 + 1;
+        auto slot_of = [&](int k) { return 2 * (size_t)(w0 + k) + (k == 0 && runs.begin(w0) < head_begin ? 1 : 0); };
+        for (int idx = tid; idx < items; idx += 256) {
+            const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
             float M = sh.m[h][0];
 #pragma unroll
             for (int w = 1; w < 4; ++w) M = fmaxf(M, sh.m[h][w]);
-            float L = 0.f, o = 0.f;
+            float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const float f = sh.m[h][w] > -INFINITY ? exp2f(sh.m[h][w] - M) : 0.f;
+                const f32x4 x = *reinterpret_cast<const f32x4*>(&sh.o[w][h][t]);
                 L += sh.l[h][w] * f;
-                o += sh.o[w][h][t] * f;
-            }
-            if (whole) { finish(h, t, o, L); continue; }
-            st_agent(&a.part_o[(slot * GP + h) * HD + t], o);
-            if (t == 0) { st_agent(&a.part_ml[(slot * GP + h) * 2], M); st_agent(&a.part_ml[(slot * GP + h) * 2 + 1], L); }
-        }
-        if (!whole) {                                               // the run that arrives last joins them all
-            const int w0 = runs.of(head_begin), w1 = runs.of(head_begin + per_head - 1);
-            wait_stores();
-            __syncthreads();
-            if (tid == 0) {
-                int* ticket = &a.tickets[b * HH + hh];
-                sh.is_last = atomicAdd(ticket, 1) == w1 - w0;
-                if (sh.is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // all arrived: leave it clean
-            }
-            __syncthreads();
-            if (sh.is_last) {
-                const size_t s0 = 2 * (size_t)w0 + (runs.begin(w0) >= head_begin ? 0 : 1);     // begins here, or in what is before
-                for (int idx = tid; idx < nh * HD; idx += 256) {
-                    const int h = idx / HD, t = idx % HD;
-                    float M = -INFINITY, L = 0.f, o = 0.f;
-                    constexpr int RND = 8;                           // partials in flight
-                    for (int w = w0; w <= w1; w += RND) {
-                        float ms[RND], ls[RND], os[RND];
 #pragma unroll
-                        for (int k = 0; k < RND; ++k) {
-                            const int ww = min(w + k, w1);
-                            const size_t p = (ww == w0 ? s0 : 2 * (size_t)ww) * GP + h;
-                            ms[k] = ld_agent(&a.part_ml[p * 2]);
-                            ls[k] = ld_agent(&a.part_ml[p * 2 + 1]);
-                            os[k] = ld_agent(&a.part_o[p * HD + t]);
+                for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
+            }
+            if (whole) finish(h, t, o, L); else publish(slot_of(run - w0), h, t, o, M, L);
+        }
+        if (!whole) {
+            constexpr int ITEMS = (kPagedHeads * (HD / 4) + 255) / 256;
+            // The run that arrives last joins them; more than kJoin in two rounds: the last of every kJoin joins these, the last of all joins what they give.
+            auto arrive = [&](int* ticket, int of) {
+                wait_stores();
+                __syncthreads();
+                if (tid == 0) {
+                    sh.is_last = atomicAdd(ticket, 1) == of - 1;
+                    if (sh.is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // all arrived: leave it clean
+                }
+                __syncthreads();
+                return sh.is_last != 0;
+            };
+            auto join = [&](int first, int step, int count, auto done) {
+#pragma unroll
+                for (int it = 0; it < ITEMS; ++it) {
+                    const int idx = tid + it * 256, h = idx / (HD / 4), t = idx % (HD / 4) * 4;
+                    if (idx >= items) break;
+                    float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int k0 = 0; k0 < count; k0 += kJoin) {
+                        float2 ml[kJoin], lo[kJoin], hi[kJoin];
+#pragma unroll
+                        for (int k = 0; k < kJoin; ++k) {
+                            const size_t p = slot_of(first + min(k0 + k, count - 1) * step) * GP + h;
+                            ml[k] = ld_agent2(&a.part_ml[p * 2]);
+                            lo[k] = ld_agent2(&a.part_o[p * HD + t]);
+                            hi[k] = ld_agent2(&a.part_o[p * HD + t + 2]);
                         }
                         float top = M;
 #pragma unroll
-                        for (int k = 0; k < RND; ++k) if (w + k <= w1) top = fmaxf(top, ms[k]);
+                        for (int k = 0; k < kJoin; ++k) if (k0 + k < count) top = fmaxf(top, ml[k].x);
                         const float keep = M > -INFINITY ? exp2f(M - top) : 0.f;
-                        L *= keep; o *= keep;
+                        L *= keep;
 #pragma unroll
-                        for (int k = 0; k < RND; ++k) {
-                            if (w + k > w1) break;
-                            const float f = ms[k] > -INFINITY ? exp2f(ms[k] - top) : 0.f;
-                            L += ls[k] * f;
-                            o += os[k] * f;
+                        for (int e = 0; e < 4; ++e) o[e] *= keep;
+#pragma unroll
+                        for (int k = 0; k < kJoin; ++k) {
+                            const float f = k0 + k < count && ml[k].x > -INFINITY ? exp2f(ml[k].x - top) : 0.f;
+                            if (k0 + k >= count) continue;
+                            L += ml[k].y * f;
+                            o[0] += lo[k].x * f; o[1] += lo[k].y * f; o[2] += hi[k].x * f; o[3] += hi[k].y * f;
                         }
                         M = top;
                     }
-                    finish(h, t, o, L);
+                    done(it, h, t, o, M, L);
+                }
+            };
+            const int sets = (parts + kJoin - 1) / kJoin, first = (run - w0) / kJoin * kJoin, count = min(kJoin, parts - first);
+            bool mine = true;
+            if (sets > 1 && count > 1) {
+                mine = arrive(&a.tickets[(size_t)a.B * HH + slot_of(first)], count);
+                if (mine) {                                         // what they give goes into the first one's slot, once all threads have read it
+                    float js[ITEMS][6];
+                    join(first, 1, count, [&](int it, int, int, const float (&o)[4], float M, float L) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) js[it][e] = o[e];
+                        js[it][4] = M; js[it][5] = L;
+                    });
+                    __syncthreads();
+#pragma unroll
+                    for (int it = 0; it < ITEMS; ++it) {
+                        const int idx = tid + it * 256;
+                        if (idx >= items) break;
+                        const float o[4] = {js[it][0], js[it][1], js[it][2], js[it][3]};
+                        publish(slot_of(first), idx / (HD / 4), idx % (HD / 4) * 4, o, js[it][4], js[it][5]);
+                    }
                 }
             }
+            if (mine && arrive(&a.tickets[b * HH + hh], sets > 1 ? sets : parts))
+                join(0, sets > 1 ? kJoin : 1, sets > 1 ? sets : parts, [&](int, int h, int t, const float (&o)[4], float, float L) { finish(h, t, o, L); });
         }
-        u += c1 - c0;
+        u = next;
         if (u < end) {
             __syncthreads();                                        // the merge has read what the next (sequence, heads) will write
             if (u == seq_begin + per_head * HH) {                   // all heads of this sequence: the next one that has rows
@@ -483,7 +554,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 
 template <typename T, int HD>
 int launch(const PagedAttnArgs& a, int n_cu, hipStream_t s) {
-    const long long most = (long long)a.B * a.H_kv * paged_head_tiles(a.group) * ((a.max_rows + PagedShape<T, HD>::CH - 1) / PagedShape<T, HD>::CH);
+    const long long most = (long long)a.B * a.H_kv * paged_head_tiles(a.group) * ((a.max_rows + PagedShape<T, HD>::CH - 1) / PagedShape<T, HD>::CH + kPagedOverhead);
     // as many workgroups as are resident, two per compute unit
     const int n = (int)std::min<long long>(most, std::min(2 * n_cu, kPagedMaxWgs));
     hipLaunchKernelGGL((attn_paged_kernel<T, HD>), dim3(n), dim3(256), 0, s, a);

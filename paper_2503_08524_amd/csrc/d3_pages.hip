@@ -32,7 +32,7 @@ int check_desc(const d3_pages_desc* d) {
     // the attention counts its chunks of work in 32 bits
     const int64_t chunks = ((int64_t)d->max_pages * d->page_rows + paged_chunk_rows(d->head_dim, d->kv_dtype) - 1) / paged_chunk_rows(d->head_dim, d->kv_dtype);
     const int64_t per_chunk = (int64_t)d->n_kv_heads * paged_head_tiles(d->n_heads / d->n_kv_heads) * d->max_batch;
-    if (chunks > INT32_MAX / per_chunk)
+    if (chunks + kPagedOverhead > INT32_MAX / per_chunk)
         return fail(D3_ESHAPE, "pages: %d sequences of up to %d pages are more rows than one attention launch counts", d->max_batch, d->max_pages);
     return D3_OK;
 }
@@ -43,7 +43,7 @@ size_t layout(const d3_pages_desc& d, size_t* part_ml, size_t* tickets) {
     const size_t partials = 2 * (size_t)kPagedMaxWgs * (group < kPagedHeads ? group : kPagedHeads);
     *part_ml = align_up(partials * d.head_dim * 4);
     *tickets = *part_ml + align_up(partials * 2 * 4);
-    return *tickets + align_up((size_t)d.max_batch * d.n_kv_heads * paged_head_tiles(group) * 4);
+    return *tickets + align_up(((size_t)d.max_batch * d.n_kv_heads * paged_head_tiles(group) + 2 * kPagedMaxWgs) * 4);
 }
 
 int check_layers(const d3_pages* p, const char* who, int32_t layer, int32_t n) {
@@ -146,7 +146,7 @@ extern "C" int d3_pages_append(d3_pages* pages, int32_t layer, int32_t n_layers,
     if (reinterpret_cast<uintptr_t>(rope_cs) % 8 != 0) return fail(D3_EINVAL, "d3_pages_append: rope_cs must be 8-byte aligned");
     const d3_pages_desc& d = pages->desc;
     AppendArgs a{};
-    a.n = n; a.n_layers = n_layers; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_rows = d.page_rows; a.n_slots = pages->n_slots();
+    a.n = n; a.n_layers = n_layers; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_shift = __builtin_ctz(d.page_rows); a.n_slots = pages->n_slots();
     a.slots = slots; a.k = k; a.v = v; a.dtype = dtype;
     a.token_stride = token_stride; a.head_stride = head_stride; a.layer_stride = layer_stride;
     a.rope_cs = reinterpret_cast<const float2*>(rope_cs);

@@ -13,6 +13,7 @@ namespace d3 {
 constexpr int kPagesMaxSeqs = 4096;        // sequences of a call
 constexpr int kPagedHeads = 16;            // query heads of one workgroup: the columns of a matrix instruction
 constexpr int kPagedMaxWgs = 1024;         // workgroups of an attention launch
+constexpr int kPagedOverhead = 1;          // what beginning and ending a (sequence, heads) costs a workgroup, in chunks
 
 // As a pool holds a value.
 template <typename T> __device__ __forceinline__ T held(float v);
@@ -29,7 +30,7 @@ struct ReserveArgs {
 int launch_pages_reserve(const ReserveArgs& a, hipStream_t s);
 
 struct AppendArgs {
-    int n, n_layers, H_kv, hd, page_rows;
+    int n, n_layers, H_kv, hd, page_shift;
     long long n_slots;                     // n_pages * page_rows
     const int32_t* slots;
     const void *k, *v;                     // [layer][token][head][dim] by the strides, in elements
@@ -64,7 +65,7 @@ struct PagedAttnArgs {
     bf16_t* out_split;                     // optional split copy
     SplitForm out_form;
     float *part_o, *part_ml;               // [2 * workgroups][min(group, 16)][hd], [..][2]
-    int* tickets;                          // [B][H_kv * tiles], zero between launches
+    int* tickets;                          // [B][H_kv * tiles], then [2 * workgroups], zero between launches
 };
 int launch_attention_paged(const PagedAttnArgs& a, int hd, int kv_dtype, int n_cu, hipStream_t s);
 // rows of a workgroup's turn: 4 waves, 16 loads of 16 bytes a lane

@@ -1,5 +1,5 @@
 // Kernels of the paged cache beside its attention: page tables and slot maps from request lengths, rows into pages, the missing-state fill on pages.
-#include <algorithm>
+#include <type_traits>
 
 #include "pages.h"
 
@@ -168,80 +168,101 @@ template <typename T> __device__ __forceinline__ void store8(T* p, const float (
     for (int e = 0; e < 8; e += 16 / sizeof(T)) *reinterpret_cast<uint4*>(p + e) = *reinterpret_cast<const uint4*>(t + e);
 }
 
-// grid: (64 tokens, KV head, layer and half: keys or values).
-// A key is a row of its page; a value's dims lie 16 bytes apart, R rows side by side.  So values pass through LDS: the token that is
-// row 0 of a unit whose R rows all follow each other in `slots` writes the unit's 16 bytes per dim for all of them, and only rows
-// of units that the call does not fill are written element by element.  Tiles read R - 1 tokens of the next one, so that units across tiles are whole.
-constexpr int kAppendTokens = 64;
+// N = 1 or 2 adjacent elements
+template <int N, typename S> __device__ __forceinline__ void load_few(const S* p, float (&y)[N]) {
+    if constexpr (N == 2 && sizeof(S) == 4) { const float2 v = *reinterpret_cast<const float2*>(p); y[0] = v.x; y[1] = v.y; }
+    else if constexpr (N == 2) {
+        const uint32_t v = *reinterpret_cast<const uint32_t*>(p);
+        S t[2];
+        __builtin_memcpy(t, &v, 4);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { if constexpr (std::is_same<S, bf16_t>::value) y[e] = bf16_to_f32(t[e]); else y[e] = (float)t[e]; }
+    } else if constexpr (std::is_same<S, bf16_t>::value) y[0] = bf16_to_f32(*p);
+    else y[0] = (float)*p;
+}
 
-template <typename S, typename T>
+// grid: (32 tokens, KV head, layer and half: keys or values); a wave has 8 tokens.
+// A key is a row of its page: eight dims of the lower half and their partners per thread.
+// Of a value's dims R rows lie side by side in 16 bytes.  A lane has one or two dims: where a token is row 0 of a unit of R rows that follow each other in
+// `slots`, its wave loads those R rows (whole lines each) and writes the unit's 16 bytes per dim, for all of them, also those of the next wave's tokens;
+// only rows of units that the call does not fill are written element by element.  What each token is, is one wave's business: bits of a mask.
+constexpr int kAppendTokens = 32;
+
+template <typename S, typename T, int HD>
 __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
-    constexpr int R = 16 / sizeof(T), TT = kAppendTokens;
-    __shared__ int slot_of[TT + 2 * (R - 1)];                      // of tokens t0 - (R - 1) .. t0 + TT + R - 2; -1: none
-    __shared__ __align__(16) T tile[(TT + R - 1) * 128];
-    const int tid = threadIdx.x, t0 = blockIdx.x * TT, h = blockIdx.y, layer = blockIdx.z >> 1, hd = a.hd, eighths = hd / 8;
+    constexpr int R = 16 / sizeof(T), DL = HD / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = blockIdx.y, layer = blockIdx.z >> 1;
     const bool values = blockIdx.z & 1;
     const S* src = static_cast<const S*>(values ? a.v : a.k) + layer * a.layer_stride + h * a.head_stride;
-    const size_t head_elems = (size_t)a.page_rows * hd;
+    const size_t head_elems = (size_t)HD << a.page_shift;
     auto pool_at = [&](void* pool, int slot) {                      // the head's rows of the slot's page
-        return reinterpret_cast<T*>(static_cast<char*>(pool) + layer * a.pool_bytes) + ((size_t)(slot / a.page_rows) * a.H_kv + h) * head_elems;
+        return reinterpret_cast<T*>(static_cast<char*>(pool) + layer * a.pool_bytes) + ((size_t)(slot >> a.page_shift) * a.H_kv + h) * head_elems;
     };
-    for (int x = tid; x < TT + 2 * (R - 1); x += 256) {
-        const int t = t0 - (R - 1) + x, slot = t >= 0 && t < a.n ? a.slots[t] : -1;
-        slot_of[x] = slot >= 0 && slot < a.n_slots ? slot : -1;
-    }
+    const int row_mask = (1 << a.page_shift) - 1;
+    auto slot_at = [&](int t) {
+        const int slot = t >= 0 && t < a.n ? a.slots[t] : -1;
+        return slot < a.n_slots ? slot : -1;
+    };
     if (!values) {
-        __syncthreads();
-        const int pairs = hd / 16;                                 // a thread has eight dims of the lower half and their partners
-        for (int x = tid; x < TT * pairs; x += 256) {
-            const int t = x / pairs, j = x % pairs * 8, slot = slot_of[t + R - 1];
+        constexpr int PER = HD / 16;                               // threads of a token
+        for (int x = tid; x < kAppendTokens * PER; x += 256) {
+            const int t = blockIdx.x * kAppendTokens + x / PER, j = x % PER * 8, slot = slot_at(t);
             if (slot < 0) continue;
             float lo[8], hi[8];
-            const S* row = src + (t0 + t) * a.token_stride;
+            const S* row = src + t * a.token_stride;
             load8<S>(row + j, lo);
-            load8<S>(row + j + hd / 2, hi);
+            load8<S>(row + j + HD / 2, hi);
             if (a.rope_cs) {
-                const float2* cs = a.rope_cs + (size_t)(t0 + t) * (hd / 2) + j;
+                float cs[16];
+                const float2* c = a.rope_cs + (size_t)t * (HD / 2) + j;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) { cs[2 * e] = c[e].x; cs[2 * e + 1] = c[e].y; }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float2 c = cs[e];
                     const float x0 = lo[e], x1 = hi[e];
-                    lo[e] = x0 * c.x - x1 * c.y;
-                    hi[e] = x1 * c.x + x0 * c.y;
+                    lo[e] = x0 * cs[2 * e] - x1 * cs[2 * e + 1];
+                    hi[e] = x1 * cs[2 * e] + x0 * cs[2 * e + 1];
                 }
             }
-            T* to = pool_at(a.k_pages, slot) + slot % a.page_rows * hd + j;
+            T* to = pool_at(a.k_pages, slot) + (slot & row_mask) * HD + j;
             store8<T>(to, lo);
-            store8<T>(to + hd / 2, hi);
+            store8<T>(to + HD / 2, hi);
         }
         return;
     }
-    const int here = min(TT + R - 1, a.n - t0);
-    for (int x = tid; x < here * eighths; x += 256) {
-        const int t = x / eighths, j = x % eighths * 8;
-        float y[8];
-        load8<S>(src + (t0 + t) * a.token_stride + j, y);
-        store8<T>(tile + t * hd + j, y);
-    }
-    __syncthreads();
-    auto fills = [&](int x) {                                      // token x of slot_of is row 0 of a unit that R tokens in a row fill
-        bool all = x >= 0 && slot_of[x] >= 0 && slot_of[x] % R == 0;
-        for (int e = 1; e < R && all; ++e) all = slot_of[x + e] == slot_of[x] + e;
-        return all;
-    };
-    for (int x = tid; x < TT * hd; x += 256) {
-        const int t = x / hd, j = x % hd, s = t + R - 1, slot = slot_of[s];
-        if (slot < 0) continue;
-        const int row = slot % a.page_rows;
-        T* to = pool_at(a.v_pages, slot) + (row / R * hd + j) * R;
-        if (fills(s)) {
+    const int t0 = blockIdx.x * kAppendTokens + wave * 8;          // this wave's tokens are t0 .. t0 + 7: lanes R - 1 .. R + 6 of the ones it looks at
+    const int slot = lane < 8 + 2 * (R - 1) ? slot_at(t0 - (R - 1) + lane) : -1;
+    const unsigned valid = (unsigned)__ballot(slot >= 0), begins = (unsigned)__ballot(slot >= 0 && slot % R == 0);
+    const int after = __shfl_down(slot, 1, 64);
+    const unsigned follows = (unsigned)__ballot(slot >= 0 && after == slot + 1);        // the next token is the next row
+    unsigned firsts = begins, covered = 0;
+#pragma unroll
+    for (int e = 0; e < R - 1; ++e) firsts &= follows >> e;
+#pragma unroll
+    for (int e = 0; e < R; ++e) covered |= firsts << e;
+    const unsigned own = 0xffu << (R - 1);
+    for (unsigned left = firsts & own; left; left &= left - 1) {
+        const int x = __builtin_ctz(left), at = __builtin_amdgcn_readlane(slot, x);
+        const S* row = src + (long long)(t0 - (R - 1) + x) * a.token_stride + lane * DL;
+        float y[R][DL];
+#pragma unroll
+        for (int e = 0; e < R; ++e) load_few<DL, S>(row + e * a.token_stride, y[e]);
+        T* to = pool_at(a.v_pages, at) + ((at & row_mask) / R * HD + lane * DL) * R;
+#pragma unroll
+        for (int d = 0; d < DL; ++d) {
             alignas(16) T unit[R];
 #pragma unroll
-            for (int e = 0; e < R; ++e) unit[e] = tile[(t + e) * hd + j];
-            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(unit);
-        } else if (!fills(s - slot % R)) {
-            to[row % R] = tile[t * hd + j];
+            for (int e = 0; e < R; ++e) unit[e] = held<T>(y[e][d]);
+            *reinterpret_cast<uint4*>(to + d * R) = *reinterpret_cast<const uint4*>(unit);
         }
+    }
+    for (unsigned left = valid & ~covered & own; left; left &= left - 1) {
+        const int x = __builtin_ctz(left), at = __builtin_amdgcn_readlane(slot, x);
+        float y[DL];
+        load_few<DL, S>(src + (long long)(t0 - (R - 1) + x) * a.token_stride + lane * DL, y);
+        T* to = pool_at(a.v_pages, at) + ((at & row_mask) / R * HD + lane * DL) * R + at % R;
+#pragma unroll
+        for (int d = 0; d < DL; ++d) to[d * R] = held<T>(y[d]);
     }
 }
 
@@ -274,13 +295,16 @@ __global__ __launch_bounds__(256) void pages_fill_kernel(PagesFillArgs a, int la
     }
 }
 
-template <typename T>
+template <typename S, typename T>
 int launch_append(const AppendArgs& a, hipStream_t s) {
     const dim3 grid((a.n + kAppendTokens - 1) / kAppendTokens, a.H_kv, 2 * a.n_layers);
-    if (a.dtype == D3_F32) hipLaunchKernelGGL((pages_append_kernel<float, T>), grid, dim3(256), 0, s, a);
-    else if (a.dtype == D3_BF16) hipLaunchKernelGGL((pages_append_kernel<bf16_t, T>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((pages_append_kernel<f16_t, T>), grid, dim3(256), 0, s, a);
+    if (a.hd == 64) hipLaunchKernelGGL((pages_append_kernel<S, T, 64>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((pages_append_kernel<S, T, 128>), grid, dim3(256), 0, s, a);
     return (int)hipGetLastError();
+}
+template <typename T>
+int launch_append_to(const AppendArgs& a, hipStream_t s) {
+    return a.dtype == D3_F32 ? launch_append<float, T>(a, s) : a.dtype == D3_BF16 ? launch_append<bf16_t, T>(a, s) : launch_append<f16_t, T>(a, s);
 }
 
 }  // namespace
@@ -296,7 +320,7 @@ int launch_pages_reserve(const ReserveArgs& a, hipStream_t s) {
 }
 
 int launch_pages_append(const AppendArgs& a, int kv_dtype, hipStream_t s) {
-    return kv_dtype == D3_F32 ? launch_append<float>(a, s) : launch_append<f16_t>(a, s);
+    return kv_dtype == D3_F32 ? launch_append_to<float>(a, s) : launch_append_to<f16_t>(a, s);
 }
 
 int launch_pages_fill(const PagesFillArgs& a, int kv_dtype, hipStream_t s) {
