@@ -271,7 +271,7 @@ int d3_pages_reserve(d3_pages *pages, int32_t B, const int32_t *added, const int
                      int32_t *slots, int32_t *positions, void *hip_stream);
 
 /* Keys and values of n tokens into their slots of `n_layers` layers from `layer` on.  k, v: dev [n_layers][n][H_kv][head_dim] of `dtype` (any of d3_dtype),
- * element (l, t, h, e) at l * layer_stride + t * token_stride + h * head_stride + e (strides in elements, multiples of 16 bytes; both pointers 16-byte aligned).  rope_cs: dev float
+ * element (l, t, h, e) at l * layer_stride + t * token_stride + h * head_stride + e (strides in elements, multiples of 16 bytes; pointers 16-byte aligned, rope_cs too).  rope_cs: dev float
  * [n][head_dim / 2][2], (cos, sin) of each token's angles, or NULL: keys turn by it (dims j and j + head_dim / 2 by angle j) before they are rounded once to the
  * pool's type. */
 int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t *slots, const void *k, const void *v, int32_t dtype,
@@ -280,7 +280,7 @@ int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n,
 /* Attention of one token per sequence over its pages: out[b][h] = softmax(scale * q[b][h] . K^T) V over rows [0, rows[b]) of sequence b; 0 where it has no row.
  * q, out: dev [B][n_heads][head_dim] of `dtype`, sequence b at b * q_stride, b * out_stride.  k_new, v_new: dev [B][H_kv][head_dim] of `dtype` at b * kv_stride, or both NULL.
  * Given, they are row rows[b] - 1, which the call also writes to its page; else that row is there already.  rope_cs: dev float [B][head_dim / 2][2]: q and
- * k_new turn by it; NULL: neither does.  q, k_new, v_new 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
+ * k_new turn by it; NULL: neither does.  q, k_new, v_new, rope_cs 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
  * Keys and values are used as the pool holds them; sums and softmax in 32 bits. */
 int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,
                        int64_t kv_stride, const float *rope_cs, const int32_t *tables, const int32_t *rows, float scale, void *out,

@@ -52,40 +52,32 @@ struct PagedShared {
 
 constexpr int kJoin = 16;      // partial results that one workgroup joins at a time, all of their loads in flight together
 
-// N consecutive activations
-template <int N>
-__device__ __forceinline__ void load_act(const void* p, long long at, int dtype, float (&y)[N]) {
-    if (dtype == D3_F32) {
-        const float* f = static_cast<const float*>(p) + at;
+// Activations as they lie in memory (A: float, or the bits of a 16-bit type) and as fp32.  The two are apart so that all loads are requested before the first conversion waits.
+template <int N, typename A>
+struct ActVec {
+    uint4 w[N * sizeof(A) >= 16 ? N * sizeof(A) / 16 : 1];         // N = 4 of 16 bits: half of it
+    __device__ __forceinline__ void load(const A* p) {
+        if constexpr (N * sizeof(A) >= 16) {
 #pragma unroll
-        for (int e = 0; e < N; e += 4) {
-            const float4 t = *reinterpret_cast<const float4*>(f + e);
-            y[e] = t.x; y[e + 1] = t.y; y[e + 2] = t.z; y[e + 3] = t.w;
-        }
-        return;
-    }
-    uint32_t w[N / 2];
-    const uint16_t* h = static_cast<const uint16_t*>(p) + at;
-    if constexpr (N == 8) {
-        const uint4 t = *reinterpret_cast<const uint4*>(h);
-        w[0] = t.x; w[1] = t.y; w[2] = t.z; w[3] = t.w;
-    } else {
-        const uint2 t = *reinterpret_cast<const uint2*>(h);
-        w[0] = t.x; w[1] = t.y;
-    }
-#pragma unroll
-    for (int e = 0; e < N; e += 2) {
-        if (dtype == D3_BF16) { y[e] = bf16_lo(w[e / 2]); y[e + 1] = bf16_hi(w[e / 2]); }
-        else {
-            y[e] = (float)__builtin_bit_cast(_Float16, (uint16_t)w[e / 2]);
-            y[e + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[e / 2] >> 16));
+            for (int j = 0; j < (int)(N * sizeof(A) / 16); ++j) w[j] = *reinterpret_cast<const uint4*>(p + j * (16 / sizeof(A)));
+        } else {
+            const uint2 t = *reinterpret_cast<const uint2*>(p);
+            w[0].x = t.x; w[0].y = t.y;
         }
     }
-}
-__device__ __forceinline__ float load_act1(const void* p, long long at, int dtype) {
-    if (dtype == D3_F32) return static_cast<const float*>(p)[at];
-    const uint16_t h = static_cast<const uint16_t*>(p)[at];
-    return dtype == D3_BF16 ? bf16_to_f32(h) : (float)__builtin_bit_cast(_Float16, h);
+    __device__ __forceinline__ void get(int dtype, float (&y)[N]) const {
+        A h[16 / sizeof(A) * sizeof(w) / 16];
+        __builtin_memcpy(h, w, sizeof(w));
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if constexpr (sizeof(A) == 4) y[e] = h[e];
+            else y[e] = dtype == D3_BF16 ? bf16_to_f32(h[e]) : (float)__builtin_bit_cast(_Float16, h[e]);
+        }
+    }
+};
+template <typename A> __device__ __forceinline__ float act_f32(A v, int dtype) {
+    if constexpr (sizeof(A) == 4) return v;
+    else return dtype == D3_BF16 ? bf16_to_f32(v) : (float)__builtin_bit_cast(_Float16, v);
 }
 // four consecutive ones; `whole`: they lie on a multiple of their size
 __device__ __forceinline__ void store_act4(void* p, long long at, int dtype, const float (&v)[4], bool whole) {
@@ -135,45 +127,67 @@ struct Runs {
     }
 };
 
-template <typename T, int HD>
+// What the first loads need of the arguments, requested together (see attn_take_args).
+__device__ __forceinline__ void paged_take_args(const PagedAttnArgs& a) {
+    asm volatile("" :: "s"(a.q), "s"(a.k_new), "s"(a.v_new), "s"(a.q_stride), "s"(a.kv_stride), "s"(a.rope_cs), "s"(a.tables), "s"(a.rows), "s"(a.table_stride),
+                       "s"(a.max_rows), "s"(a.B), "s"(a.H_kv), "s"(a.group), "s"(a.n_pages), "s"(a.page_shift), "s"(a.k_pages), "s"(a.v_pages));
+    asm volatile("" :: "s"(a.dtype), "s"(a.scale), "s"(a.out), "s"(a.out_stride), "s"(a.out_split), "s"(a.out_form.lo), "s"(a.part_o), "s"(a.part_ml), "s"(a.tickets));
+}
+
+// T: the pool's type; A: float, or the bits of a 16-bit type (q, k_new, v_new)
+template <typename T, int HD, typename A>
 __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
     typedef PagedShape<T, HD> P;
     constexpr int R = P::R, KT = P::KT, RG = P::RG, NK = P::NK, ND = P::ND, U = P::U, QE = P::QE;
     __shared__ PagedShared<T, HD> sh;
+    paged_take_args(a);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
     const int H = a.H_kv * a.group, tiles = (a.group + kPagedHeads - 1) / kPagedHeads, HH = a.H_kv * tiles, GP = min(a.group, kPagedHeads);
     auto length = [&](int b) { return min(max(a.rows[b], 0), a.max_rows); };
 
     // ---- this workgroup's run of units, and where it begins ----
-    auto units_of = [&](int b) {
-        const int len = b < a.B ? length(b) : 0;
-        return len > 0 ? ((len + P::CH - 1) / P::CH + kPagedOverhead) * HH : 0;
-    };
-    int n = units_of(lane), upto = scan_wave(n), total = __builtin_amdgcn_readlane(upto, 63);
-    const int total64 = total;
-    for (int b0 = 64; b0 < a.B; b0 += 64) total += __builtin_amdgcn_readlane(scan_wave(units_of(b0 + lane)), 63);
-    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {             // a sequence without rows: zeros
-        if (length(b) > 0) continue;
-        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int e = tid * 4; e < H * HD; e += 1024) {
-            store_act4(a.out, b * a.out_stride + e, a.dtype, zero, false);
-            if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H * HD), e, zero, a.out_form.lo);
+    // Lane x has sequence b0 + x.  A (sequence, heads) counts as its chunks, and where runs are longer than the shortest one, i.e. may hold several, as `over` more: what beginning
+    // and ending it costs (48 requests of 1 to 32768 rows 130 -> 110 us).  Elsewhere that would only make runs uneven (20480 rows, 32 heads: 160 chunks are 10 a workgroup; 57.8 us, with `over` 62.3).
+    int len_of = lane < a.B ? length(lane) : 0;
+    int total = 0, live = 0;
+    float shortest = INFINITY;                                      // of up to 2^24 chunks
+    bool idle = false;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        const int len = b0 == 0 ? len_of : b0 + lane < a.B ? length(b0 + lane) : 0, c = (len + P::CH - 1) / P::CH;
+        total += __builtin_amdgcn_readlane(scan_wave(c), 63);
+        live += __popcll(__ballot(len > 0));
+        idle = idle || __any(b0 + lane < a.B && len == 0);
+        shortest = fminf(shortest, -reduce_row(reduce_row_pairs(reduce_halves(len > 0 ? -(float)c : -INFINITY, MaxOp()), MaxOp()), MaxOp()));
+    }
+    const int over = (float)(total * HH / (int)gridDim.x) > __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(shortest))) ? kPagedOverhead : 0;
+    total = (total + live * over) * HH;
+    if (idle) {
+        for (int b = blockIdx.x; b < a.B; b += gridDim.x) {         // a sequence without rows: zeros
+            if (length(b) > 0) continue;
+            const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int e = tid * 4; e < H * HD; e += 1024) {
+                store_act4(a.out, b * a.out_stride + e, a.dtype, zero, false);
+                if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H * HD), e, zero, a.out_form.lo);
+            }
         }
     }
     const Runs runs(total, gridDim.x);
     const int run = blockIdx.x, end = runs.begin(run + 1);
     int u = runs.begin(run);
     if (u >= end) return;
-    int b = 0, seq_begin = 0;                                       // the sequence of unit u, and its first unit
-    {
-        int before = 0, b0 = 0, here = total64;
-        while (u >= before + here) {
-            before += here; b0 += 64;
-            n = units_of(b0 + lane); upto = scan_wave(n); here = __builtin_amdgcn_readlane(upto, 63);
+    int b = 0, seq_begin = 0, len = 0;                              // the sequence of unit u, its first unit and its rows
+    for (int b0 = 0, before = 0;; b0 += 64) {
+        if (b0 > 0) len_of = b0 + lane < a.B ? length(b0 + lane) : 0;
+        const int n = len_of > 0 ? ((len_of + P::CH - 1) / P::CH + over) * HH : 0, upto = before + scan_wave(n);
+        const unsigned long long past = __ballot(upto > u);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            b = b0 + at;
+            seq_begin = __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at);
+            len = __builtin_amdgcn_readlane(len_of, at);
+            break;
         }
-        const int at = __builtin_ctzll(__ballot(before + upto > u));
-        b = b0 + at;
-        seq_begin = before + __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at);
+        before = __builtin_amdgcn_readlane(upto, 63);
     }
 
     const int block_shift = a.page_shift - (R == 8 ? 3 : 2), block_mask = (1 << block_shift) - 1;      // blocks of R rows
@@ -181,11 +195,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
     const bool out_whole = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_stride % 4 == 0;
 
     while (u < end) {
-        const int len = __builtin_amdgcn_readfirstlane(length(b));
-        const int chunks = (len + P::CH - 1) / P::CH, per_head = chunks + kPagedOverhead, hh = (u - seq_begin) / per_head, head_begin = seq_begin + hh * per_head;
-        const int c0 = max(u - head_begin - kPagedOverhead, 0), c1 = min(chunks, end - head_begin - kPagedOverhead);
+        const int chunks = (len + P::CH - 1) / P::CH, per_head = chunks + over, hh = (u - seq_begin) / per_head, head_begin = seq_begin + hh * per_head;
+        const int c0 = max(u - head_begin - over, 0), c1 = min(chunks, end - head_begin - over);
         const int next = min(end, head_begin + per_head);
-        if (c1 <= 0) return;                                        // the run ends in the overhead of this one
+        if (c1 <= 0) return;                                        // the run ends in what this one counts more
         const int kvh = hh / tiles, h0 = (hh - kvh * tiles) * kPagedHeads, nh = min(kPagedHeads, a.group - h0);
         const bool whole = c0 == 0 && c1 == chunks;
         const int newest = len - 1, last_block = newest / R;
@@ -225,21 +238,6 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                 for (int d = 0; d < ND; ++d) vr[x][d] = __builtin_bit_cast(uint4, load_stream16(p + d * 256));
             }
         };
-        // dims of piece k that this lane has of q and of a new key: k * 4 QE + g * QE ...; those half a head away are the lane's too
-        auto rotated = [&](float (&y)[NK][QE]) {
-#pragma unroll
-            for (int k = 0; k < NK / 2; ++k) {
-                const float2* cs = a.rope_cs + (size_t)b * (HD / 2) + k * 4 * QE + g * QE;
-#pragma unroll
-                for (int e = 0; e < QE; ++e) {
-                    const float2 t = cs[e];
-                    const float lo = y[k][e], hi = y[k + NK / 2][e];
-                    y[k][e] = lo * t.x - hi * t.y;
-                    y[k + NK / 2][e] = hi * t.x + lo * t.y;
-                }
-            }
-        };
-
         // the wave whose turn has the newest row rounds it as the pool does, and puts it into its page
         const bool fresh = a.k_new && c1 == chunks && (newest / P::TR & 3) == wave;
         float m = -INFINITY, l = 0.f;
@@ -247,39 +245,66 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (r < rend) {
-            float2 nk = {0.f, 0.f}, nv = {0.f, 0.f}, ncs = {1.f, 0.f};      // dims `lane` and lane + HD / 2 of the newest row
-            if (fresh && lane < HD / 2) {
-                const long long at = b * a.kv_stride + (long long)kvh * HD + lane;
-                nk = make_float2(load_act1(a.k_new, at, a.dtype), load_act1(a.k_new, at + HD / 2, a.dtype));
-                nv = make_float2(load_act1(a.v_new, at, a.dtype), load_act1(a.v_new, at + HD / 2, a.dtype));
-                if (a.rope_cs) ncs = a.rope_cs[(size_t)b * (HD / 2) + lane];
+            A nk[2], nv[2];                                         // dims `lane` and lane + HD / 2 of the newest row
+            float2 ncs = {1.f, 0.f};
+            if (fresh) {
+                const long long at = b * a.kv_stride + (long long)kvh * HD + lane % (HD / 2);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    nk[e] = static_cast<const A*>(a.k_new)[at + e * (HD / 2)];
+                    nv[e] = static_cast<const A*>(a.v_new)[at + e * (HD / 2)];
+                }
+                if (a.rope_cs) ncs = a.rope_cs[(size_t)b * (HD / 2) + lane % (HD / 2)];
             }
             int pk[U], pv[U], pk1[U], pv1[U];
             load_pages(r, pk, pv);
             load_pages(r + P::CH, pk1, pv1);
             float qf[NK][QE];
+            ActVec<QE, A> qa[NK];
 #pragma unroll
-            for (int k = 0; k < NK; ++k) load_act<QE>(a.q, b * a.q_stride + (long long)(kvh * a.group + h0 + min(i, nh - 1)) * HD + k * 4 * QE + g * QE, a.dtype, qf[k]);
+            for (int k = 0; k < NK; ++k) qa[k].load(static_cast<const A*>(a.q) + b * a.q_stride + (long long)(kvh * a.group + h0 + min(i, nh - 1)) * HD + k * 4 * QE + g * QE);
+            // a lane has dims k * 4 QE + g * QE ... of q, k < NK: those half a head away, with which they turn, among them
+            ActVec<2 * QE, float> cs[NK / 2];
+            if (a.rope_cs) {
+#pragma unroll
+                for (int k = 0; k < NK / 2; ++k) cs[k].load(reinterpret_cast<const float*>(a.rope_cs + (size_t)b * (HD / 2) + k * 4 * QE + g * QE));
+            }
+            const int new_page = tab[last_block >> block_shift];
+            __builtin_amdgcn_sched_barrier(0);
             issue_k(r, pk);
             issue_v(r, pv);
             __builtin_amdgcn_sched_barrier(0);
             if (fresh) {
-                const int page = tab[last_block >> block_shift];
                 if (lane < HD / 2) {
-                    const float y[2] = {nk.x * ncs.x - nk.y * ncs.y, nk.y * ncs.x + nk.x * ncs.y}, z[2] = {nv.x, nv.y};
+                    const float k0 = act_f32(nk[0], a.dtype), k1 = act_f32(nk[1], a.dtype);
+                    const float y[2] = {k0 * ncs.x - k1 * ncs.y, k1 * ncs.x + k0 * ncs.y}, z[2] = {act_f32(nv[0], a.dtype), act_f32(nv[1], a.dtype)};
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int d = lane + e * (HD / 2);
                         const T kt = held<T>(y[e]), vt = held<T>(z[e]);
                         sh.new_k[d] = kt; sh.new_v[d] = vt;
-                        if (h0 == 0 && present(page)) {
-                            reinterpret_cast<T*>(Kh + page * page_bytes)[(newest & ((1 << a.page_shift) - 1)) * HD + d] = kt;
-                            reinterpret_cast<T*>(Vh + page * page_bytes)[((last_block & block_mask) * HD + d) * R + newest % R] = vt;
+                        if (h0 == 0 && present(new_page)) {
+                            reinterpret_cast<T*>(Kh + new_page * page_bytes)[(newest & ((1 << a.page_shift) - 1)) * HD + d] = kt;
+                            reinterpret_cast<T*>(Vh + new_page * page_bytes)[((last_block & block_mask) * HD + d) * R + newest % R] = vt;
                         }
                     }
                 }
             }
-            if (a.rope_cs) rotated(qf);
+#pragma unroll
+            for (int k = 0; k < NK; ++k) qa[k].get(a.dtype, qf[k]);
+            if (a.rope_cs) {
+#pragma unroll
+                for (int k = 0; k < NK / 2; ++k) {
+                    float c[2 * QE];
+                    cs[k].get(D3_F32, c);
+#pragma unroll
+                    for (int e = 0; e < QE; ++e) {
+                        const float lo = qf[k][e], hi = qf[k + NK / 2][e];
+                        qf[k][e] = lo * c[2 * e] - hi * c[2 * e + 1];
+                        qf[k + NK / 2][e] = hi * c[2 * e] + lo * c[2 * e + 1];
+                    }
+                }
+            }
             // q as fp16 halves hi + lo, scaled by a power of two that puts its largest element at 2^14: 22 bits of it
             float mul = a.scale * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
             half8 qh[NK], ql[NK];
@@ -437,23 +462,31 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(&sh.o[wave][i][d * 16 + g * 4]) = acc[d];
         }
         __syncthreads();
+        // From here on addresses are computed where they are used (the compiler cannot know that `none` is 0): ahead of the loop over (sequence, heads), where it would compute
+        // them, every launch waits for them before its first load, and they spill.
+        int none = 0;
+        asm volatile("" : "+s"(none));
+        const int H_ = H + none, HH_ = HH + none, GP_ = GP + none;
         const int items = nh * (HD / 4);                            // a thread has four dims of a head
         auto finish = [&](int h, int t, const float (&o)[4], float sum) {
             const float by = sum == 0.f ? 0.f : 1.f / sum;          // no row counted: zeros
             const float v[4] = {o[0] * by, o[1] * by, o[2] * by, o[3] * by};
             const int e = (kvh * a.group + h0 + h) * HD + t;
             store_act4(a.out, b * a.out_stride + e, a.dtype, v, out_whole);
-            if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H * HD), e, v, a.out_form.lo);
+            if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H_ * HD), e, v, a.out_form.lo);
         };
-        auto publish = [&](size_t slot, int h, int t, const float (&o)[4], float M, float L) {
-            float* p = &a.part_o[(slot * GP + h) * HD + t];
-            st_agent2(p, o[0], o[1]);
-            st_agent2(p + 2, o[2], o[3]);
-            if (t == 0) st_agent2(&a.part_ml[(slot * GP + h) * 2], M, L);
+        // (32-bit offsets: the partial results of all runs are 16 MiB at most)
+        auto part_o_at = [&](unsigned slot, int h, int t) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_o) + ((slot * GP_ + h) * HD + t) * 4u); };
+        auto part_ml_at = [&](unsigned slot, int h) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_ml) + (slot * GP_ + h) * 8u); };
+        auto publish = [&](unsigned slot, int h, int t, const float (&o)[4], float M, float L) {
+            st_agent2(part_o_at(slot, h, t), o[0], o[1]);
+            st_agent2(part_o_at(slot, h, t + 2), o[2], o[3]);
+            if (t == 0) st_agent2(part_ml_at(slot, h), M, L);
         };
         // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
-        const int w0 = runs.of(head_begin + kPagedOverhead), w1 = runs.of(head_begin + per_head - 1), parts = w1 - w0 + 1;
-        auto slot_of = [&](int k) { return 2 * (size_t)(w0 + k) + (k == 0 && runs.begin(w0) < head_begin ? 1 : 0); };
+        const int w0 = runs.of(head_begin + over), w1 = runs.of(head_begin + per_head - 1), parts = w1 - w0 + 1;
+        const unsigned before = runs.begin(w0) < head_begin ? 1 : 0;
+        auto slot_of = [&](int k) { return 2u * (w0 + k) + (k == 0 ? before : 0); };
         for (int idx = tid; idx < items; idx += 256) {
             const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
             float M = sh.m[h][0];
@@ -462,7 +495,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float f = sh.m[h][w] > -INFINITY ? exp2f(sh.m[h][w] - M) : 0.f;
+                const float f = sh.m[h][w] > -INFINITY ? __builtin_amdgcn_exp2f(sh.m[h][w] - M) : 0.f;
                 const f32x4 x = *reinterpret_cast<const f32x4*>(&sh.o[w][h][t]);
                 L += sh.l[h][w] * f;
 #pragma unroll
@@ -493,22 +526,24 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         float2 ml[kJoin], lo[kJoin], hi[kJoin];
 #pragma unroll
                         for (int k = 0; k < kJoin; ++k) {
-                            const size_t p = slot_of(first + min(k0 + k, count - 1) * step) * GP + h;
-                            ml[k] = ld_agent2(&a.part_ml[p * 2]);
-                            lo[k] = ld_agent2(&a.part_o[p * HD + t]);
-                            hi[k] = ld_agent2(&a.part_o[p * HD + t + 2]);
+                            const unsigned slot = slot_of(first + min(k0 + k, count - 1) * step);
+                            ml[k] = ld_agent2(part_ml_at(slot, h));
+                            lo[k] = ld_agent2(part_o_at(slot, h, t));
+                            hi[k] = ld_agent2(part_o_at(slot, h, t + 2));
                         }
                         float top = M;
 #pragma unroll
-                        for (int k = 0; k < kJoin; ++k) if (k0 + k < count) top = fmaxf(top, ml[k].x);
-                        const float keep = M > -INFINITY ? exp2f(M - top) : 0.f;
+                        for (int k = 0; k < kJoin; ++k) {
+                            if (k0 + k >= count) { ml[k] = make_float2(-INFINITY, 0.f); lo[k] = hi[k] = make_float2(0.f, 0.f); }
+                            top = fmaxf(top, ml[k].x);
+                        }
+                        const float keep = M > -INFINITY ? __builtin_amdgcn_exp2f(M - top) : 0.f;
                         L *= keep;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) o[e] *= keep;
 #pragma unroll
                         for (int k = 0; k < kJoin; ++k) {
-                            const float f = k0 + k < count && ml[k].x > -INFINITY ? exp2f(ml[k].x - top) : 0.f;
-                            if (k0 + k >= count) continue;
+                            const float f = ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - top) : 0.f;
                             L += ml[k].y * f;
                             o[0] += lo[k].x * f; o[1] += lo[k].y * f; o[2] += hi[k].x * f; o[3] += hi[k].y * f;
                         }
@@ -520,7 +555,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             const int sets = (parts + kJoin - 1) / kJoin, first = (run - w0) / kJoin * kJoin, count = min(kJoin, parts - first);
             bool mine = true;
             if (sets > 1 && count > 1) {
-                mine = arrive(&a.tickets[(size_t)a.B * HH + slot_of(first)], count);
+                mine = arrive(&a.tickets[a.B * HH_ + (int)slot_of(first)], count);
                 if (mine) {                                         // what they give goes into the first one's slot, once all threads have read it
                     float js[ITEMS][6];
                     join(first, 1, count, [&](int it, int, int, const float (&o)[4], float M, float L) {
@@ -538,7 +573,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                     }
                 }
             }
-            if (mine && arrive(&a.tickets[b * HH + hh], sets > 1 ? sets : parts))
+            if (mine && arrive(&a.tickets[b * HH_ + hh], sets > 1 ? sets : parts))
                 join(0, sets > 1 ? kJoin : 1, sets > 1 ? sets : parts, [&](int, int h, int t, const float (&o)[4], float, float L) { finish(h, t, o, L); });
         }
         u = next;
@@ -546,7 +581,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             __syncthreads();                                        // the merge has read what the next (sequence, heads) will write
             if (u == seq_begin + per_head * HH) {                   // all heads of this sequence: the next one that has rows
                 seq_begin = u;
-                do ++b; while (length(b) == 0);                     // there is one: u < end <= total
+                do len = __builtin_amdgcn_readfirstlane(length(++b)); while (len == 0);      // there is one: u < end <= total
             }
         }
     }
@@ -554,10 +589,11 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 
 template <typename T, int HD>
 int launch(const PagedAttnArgs& a, int n_cu, hipStream_t s) {
-    const long long most = (long long)a.B * a.H_kv * paged_head_tiles(a.group) * ((a.max_rows + PagedShape<T, HD>::CH - 1) / PagedShape<T, HD>::CH + kPagedOverhead);
+    const long long most = (long long)a.B * a.H_kv * paged_head_tiles(a.group) * ((a.max_rows + PagedShape<T, HD>::CH - 1) / PagedShape<T, HD>::CH);
     // as many workgroups as are resident, two per compute unit
     const int n = (int)std::min<long long>(most, std::min(2 * n_cu, kPagedMaxWgs));
-    hipLaunchKernelGGL((attn_paged_kernel<T, HD>), dim3(n), dim3(256), 0, s, a);
+    if (a.dtype == D3_F32) hipLaunchKernelGGL((attn_paged_kernel<T, HD, float>), dim3(n), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_paged_kernel<T, HD, uint16_t>), dim3(n), dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
 

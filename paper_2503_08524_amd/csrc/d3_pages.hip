@@ -143,7 +143,7 @@ extern "C" int d3_pages_append(d3_pages* pages, int32_t layer, int32_t n_layers,
     const int unit = 16 / elem_bytes(dtype);
     if (!aligned16(k) || !aligned16(v) || token_stride % unit != 0 || head_stride % unit != 0 || layer_stride % unit != 0)
         return fail(D3_EINVAL, "d3_pages_append: k, v and their strides must be multiples of 16 bytes");
-    if (reinterpret_cast<uintptr_t>(rope_cs) % 8 != 0) return fail(D3_EINVAL, "d3_pages_append: rope_cs must be 8-byte aligned");
+    if (!aligned16(rope_cs)) return fail(D3_EINVAL, "d3_pages_append: rope_cs must be 16-byte aligned");
     const d3_pages_desc& d = pages->desc;
     AppendArgs a{};
     a.n = n; a.n_layers = n_layers; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_shift = __builtin_ctz(d.page_rows); a.n_slots = pages->n_slots();
@@ -168,7 +168,7 @@ extern "C" int d3_pages_attention(d3_pages* pages, int32_t layer, int32_t B, con
     const int unit = 16 / elem_bytes(dtype);
     if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || q_stride % unit != 0 || (k_new && kv_stride % unit != 0))
         return fail(D3_EINVAL, "d3_pages_attention: q, k_new, v_new and their strides must be multiples of 16 bytes");
-    if (reinterpret_cast<uintptr_t>(rope_cs) % 8 != 0) return fail(D3_EINVAL, "d3_pages_attention: rope_cs must be 8-byte aligned");
+    if (!aligned16(rope_cs)) return fail(D3_EINVAL, "d3_pages_attention: rope_cs must be 16-byte aligned");
     if (!(scale - scale == 0.f)) return fail(D3_EINVAL, "d3_pages_attention: scale must be finite");
     PagedAttnArgs a = paged_attn_args(pages, layer, B);
     a.q = q; a.k_new = k_new; a.v_new = v_new; a.dtype = dtype;
