@@ -327,6 +327,10 @@ class PagedCache:
         if ws_bytes == 0:
             raise D3Error(-2, self.lib.d3_last_error().decode())
         self._kinds = {torch.float32: D3_F32, torch.bfloat16: D3_BF16, torch.float16: D3_F16}
+        self._int32, self._float32 = torch.int32, torch.float32
+        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        # the current stream's handle without the object around it (2 us a call), where torch offers that
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
         tdt = {"f32": torch.float32, "f16": torch.float16}[kv_dtype]
         unit = 16 // tdt.itemsize
         with torch.cuda.device(self.device):
@@ -356,26 +360,34 @@ class PagedCache:
 
     __del__ = close
 
+    # (A decode step makes a few of these calls per block, so their checks look at each tensor once.)
     def _stream(self) -> int:
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+        return self._raw_stream(self._index)
 
     def _ints(self, **tensors) -> None:
         for name, t in tensors.items():
-            if t.dtype != self.torch.int32 or t.device != self.device or not t.is_contiguous():
+            if t.dtype is not self._int32 or t.get_device() != self._index or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 tensor on {self.device}")
 
     def _angles(self, rope_cs, n: int) -> Optional[int]:
         if rope_cs is None:
             return None
-        if rope_cs.dtype != self.torch.float32 or rope_cs.device != self.device or not rope_cs.is_contiguous() or tuple(rope_cs.shape) != (n, self.head_dim // 2, 2):
+        if rope_cs.shape != (n, self.head_dim // 2, 2) or rope_cs.dtype is not self._float32 or rope_cs.get_device() != self._index or not rope_cs.is_contiguous():
             raise ValueError(f"rope_cs must be a contiguous float32 tensor ({n}, {self.head_dim // 2}, 2) on {self.device}")
         return rope_cs.data_ptr()
 
-    def _heads(self, name: str, t, dims):
-        """The tensor's dtype as d3_dtype; its last dim must be dense."""
-        if tuple(t.shape) != tuple(dims) or t.device != self.device or t.dtype not in self._kinds or t.stride(-1) != 1:
-            raise ValueError(f"{name} must be a float32, bfloat16 or float16 tensor {tuple(dims)} on {self.device} whose last dim is dense")
-        return self._kinds[t.dtype]
+    def _heads(self, name: str, t, dims, dtype, strides=None):
+        """The tensor's strides; it must have these dims, this dtype, a dense last dim (and these strides)."""
+        own = t.stride()
+        if t.shape != dims or t.dtype is not dtype or t.get_device() != self._index or own[-1] != 1 or (strides is not None and own != strides):
+            raise ValueError(f"{name} must be a {dtype} tensor {tuple(dims)} on {self.device}, its last dim dense{'' if strides is None else f', with strides {strides}'}")
+        return own
+
+    def _kind(self, t) -> int:
+        kind = self._kinds.get(t.dtype)
+        if kind is None:
+            raise ValueError(f"keys, values and queries must be float32, bfloat16 or float16 (got {t.dtype})")
+        return kind
 
     def reserve(self, added, max_tokens: int, starts=None, slots=None, positions=None, rows_out=None, n_free_out=None):
         """Room for added[b] more rows of sequence b (int32 CUDA tensor [B]; 0: none, negative: the sequence has ended), B <= max_batch, at most max_tokens rows in all.
@@ -401,41 +413,39 @@ class PagedCache:
     def append(self, layer: int, slots, k, v, rope_cs=None) -> None:
         """k, v [n][n_kv_heads][head_dim], or [m][n][n_kv_heads][head_dim] for the m layers from `layer` on, into the rows `slots` (int32 CUDA tensor [n]) of the pools.
         rope_cs [n][head_dim / 2][2]: (cos, sin) by which the keys turn first."""
-        if k.dim() == 3:
-            k, v = k[None], v[None]
-        n, layers = slots.numel(), k.shape[0]
-        dims = (layers, n, self.n_kv_heads, self.head_dim)
-        kind = self._heads("k", k, dims)
-        self._heads("v", v, dims)
         self._ints(slots=slots)
-        if k.dtype != v.dtype or k.stride() != v.stride():
-            raise ValueError("k and v must have one dtype and the same strides")
-        _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, k.stride(1), k.stride(2), k.stride(0),
-                                        self._angles(rope_cs, n), self._stream()))
+        n, kind = slots.numel(), self._kind(k)
+        layers = k.shape[0] if k.dim() == 4 else 1
+        dims = (layers, n, self.n_kv_heads, self.head_dim) if k.dim() == 4 else (n, self.n_kv_heads, self.head_dim)
+        strides = self._heads("k", k, dims, k.dtype)
+        self._heads("v", v, dims, k.dtype, strides)
+        _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, strides[-3], strides[-2],
+                                        strides[0] if len(strides) == 4 else 0, self._angles(rope_cs, n), self._stream()))
 
     def attend(self, layer: int, q, k=None, v=None, rope_cs=None, scale: float = 0.0, out=None):
         """Attention of one token of each of the first B sequences, q [B][n_heads][head_dim], over their rows; returns out [B][n_heads][head_dim] of q's dtype.
         k, v [B][n_kv_heads][head_dim]: the newest rows (row rows[b] - 1), which the call also writes to their pages; without them they are there already.
         rope_cs [B][head_dim / 2][2]: q and k turn by it.  scale 0: 1 / sqrt(head_dim)."""
-        B = q.shape[0]
+        B, dtype, kind = q.shape[0], q.dtype, self._kind(q)
         dims = (B, self.n_heads, self.head_dim)
-        kind = self._heads("q", q, dims)
         if out is None:
-            out = self.torch.empty(dims, dtype=q.dtype, device=self.device)
-        self._heads("out", out, dims)
-        if out.dtype != q.dtype or q.stride(1) != self.head_dim or out.stride(1) != self.head_dim:
-            raise ValueError("q and out must have one dtype and the heads of a sequence side by side")
-        if (k is None) != (v is None):
+            out = self.torch.empty(dims, dtype=dtype, device=self.device)
+        q_strides, out_strides = self._heads("q", q, dims, dtype), self._heads("out", out, dims, dtype)
+        if q_strides[1] != self.head_dim or out_strides[1] != self.head_dim:
+            raise ValueError("q and out must have the heads of a sequence side by side")
+        k_at = v_at = None
+        kv_strides = (0,)
+        if k is not None and v is not None:
+            dims = (B, self.n_kv_heads, self.head_dim)
+            kv_strides = self._heads("k", k, dims, dtype)
+            self._heads("v", v, dims, dtype, kv_strides)
+            if kv_strides[1] != self.head_dim:
+                raise ValueError("k and v must have the heads of a sequence side by side")
+            k_at, v_at = k.data_ptr(), v.data_ptr()
+        elif k is not None or v is not None:
             raise ValueError("k and v come together or not at all")
-        kv_stride = 0
-        if k is not None:
-            self._heads("k", k, (B, self.n_kv_heads, self.head_dim))
-            self._heads("v", v, (B, self.n_kv_heads, self.head_dim))
-            if k.dtype != q.dtype or v.dtype != q.dtype or k.stride() != v.stride() or k.stride(1) != self.head_dim:
-                raise ValueError("k and v must have q's dtype, the same strides and the heads of a sequence side by side")
-            kv_stride = k.stride(0)
-        _check(self.lib.d3_pages_attention(self.handle, layer, B, q.data_ptr(), _ptr(k), _ptr(v), kind, q.stride(0), kv_stride, self._angles(rope_cs, B),
-                                           self.tables.data_ptr(), self.rows.data_ptr(), scale, out.data_ptr(), out.stride(0), self._stream()))
+        _check(self.lib.d3_pages_attention(self.handle, layer, B, q.data_ptr(), k_at, v_at, kind, q_strides[0], kv_strides[0], self._angles(rope_cs, B),
+                                           self.tables.data_ptr(), self.rows.data_ptr(), scale, out.data_ptr(), out_strides[0], self._stream()))
         return out
 
     def fill(self, slots, src: int, first: int, n_layers: int) -> None:

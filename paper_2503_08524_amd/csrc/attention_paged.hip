@@ -43,7 +43,7 @@ struct PagedShape {
 };
 
 template <typename T, int HD>
-struct PagedShared {
+struct __align__(16) PagedShared {
     float o[4][kPagedHeads][HD + 4];               // per wave: unnormalised outputs (rows 4 words apart in the banks)
     float m[kPagedHeads][4], l[kPagedHeads][4];    // per wave: running max and sum of each head
     T new_k[HD], new_v[HD];                        // the newest row as the pool holds it
@@ -116,14 +116,22 @@ __device__ __forceinline__ int scan_wave(int v) {                  // inclusive:
     return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
 }
 
-// Equal runs of `total` units: the first `over` workgroups have one more.
+// x / d where the quotient is below 2^20 (an estimate that is one off at most, and a correction): a division is 40 dependent instructions.
+__device__ __forceinline__ int small_quotient(int x, int d) {
+    int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
+    const int r = x - q * d;
+    q += r >= d ? 1 : r < 0 ? -1 : 0;
+    return __builtin_amdgcn_readfirstlane(q);
+}
+
+// Equal runs of `total` units: the first `more` workgroups have one more.
 struct Runs {
-    int per, over;
-    __device__ Runs(int total, int n) : per((int)((unsigned)total / (unsigned)n)), over(total - per * n) {}
-    __device__ int begin(int w) const { return w * per + min(w, over); }
+    int per, more;
+    __device__ Runs(int total, const Divisor& by) : per(by.of(total)), more(total - per * by.d) {}
+    __device__ int begin(int w) const { return w * per + min(w, more); }
     __device__ int of(int x) const {                               // the run that unit x is in
-        const int larger = over * (per + 1);
-        return x < larger ? x / (per + 1) : over + (x - larger) / per;      // per = 0: every unit is below `larger`
+        const int larger = more * (per + 1);
+        return x < larger ? small_quotient(x, per + 1) : more + small_quotient(x - larger, max(per, 1));      // per = 0: every unit is below `larger`
     }
 };
 
@@ -131,7 +139,7 @@ struct Runs {
 __device__ __forceinline__ void paged_take_args(const PagedAttnArgs& a) {
     asm volatile("" :: "s"(a.q), "s"(a.k_new), "s"(a.v_new), "s"(a.q_stride), "s"(a.kv_stride), "s"(a.rope_cs), "s"(a.tables), "s"(a.rows), "s"(a.table_stride),
                        "s"(a.max_rows), "s"(a.B), "s"(a.H_kv), "s"(a.group), "s"(a.n_pages), "s"(a.page_shift), "s"(a.k_pages), "s"(a.v_pages));
-    asm volatile("" :: "s"(a.dtype), "s"(a.scale), "s"(a.out), "s"(a.out_stride), "s"(a.out_split), "s"(a.out_form.lo), "s"(a.part_o), "s"(a.part_ml), "s"(a.tickets));
+    asm volatile("" :: "s"(a.dtype), "s"(a.scale), "s"(a.out), "s"(a.out_stride), "s"(a.out_split), "s"(a.out_form.lo), "s"(a.part_o), "s"(a.part_ml), "s"(a.tickets), "s"(a.by_runs.d), "s"(a.by_runs.m));
 }
 
 // T: the pool's type; A: float, or the bits of a 16-bit type (q, k_new, v_new)
@@ -159,7 +167,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
         idle = idle || __any(b0 + lane < a.B && len == 0);
         shortest = fminf(shortest, -reduce_row(reduce_row_pairs(reduce_halves(len > 0 ? -(float)c : -INFINITY, MaxOp()), MaxOp()), MaxOp()));
     }
-    const int over = (float)(total * HH / (int)gridDim.x) > __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(shortest))) ? kPagedOverhead : 0;
+    const int over = (float)(total * HH) > (float)gridDim.x * __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(shortest))) ? kPagedOverhead : 0;
     total = (total + live * over) * HH;
     if (idle) {
         for (int b = blockIdx.x; b < a.B; b += gridDim.x) {         // a sequence without rows: zeros
@@ -171,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             }
         }
     }
-    const Runs runs(total, gridDim.x);
+    const Runs runs(total, a.by_runs);
     const int run = blockIdx.x, end = runs.begin(run + 1);
     int u = runs.begin(run);
     if (u >= end) return;
@@ -195,12 +203,16 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
     const bool out_whole = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_stride % 4 == 0;
 
     while (u < end) {
-        const int chunks = (len + P::CH - 1) / P::CH, per_head = chunks + over, hh = (u - seq_begin) / per_head, head_begin = seq_begin + hh * per_head;
+        const int chunks = (len + P::CH - 1) / P::CH, per_head = chunks + over, hh = small_quotient(u - seq_begin, per_head), head_begin = seq_begin + hh * per_head;
         const int c0 = max(u - head_begin - over, 0), c1 = min(chunks, end - head_begin - over);
         const int next = min(end, head_begin + per_head);
         if (c1 <= 0) return;                                        // the run ends in what this one counts more
-        const int kvh = hh / tiles, h0 = (hh - kvh * tiles) * kPagedHeads, nh = min(kPagedHeads, a.group - h0);
+        const int kvh = tiles == 1 ? hh : small_quotient(hh, tiles), h0 = (hh - kvh * tiles) * kPagedHeads, nh = min(kPagedHeads, a.group - h0);
         const bool whole = c0 == 0 && c1 == chunks;
+        // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
+        const int w0 = whole ? run : runs.of(head_begin + over), parts = whole ? 1 : runs.of(head_begin + per_head - 1) - w0 + 1;
+        const unsigned before = runs.begin(w0) < head_begin ? 1 : 0;
+        auto slot_of = [&](int k) { return 2u * (w0 + k) + (k == 0 ? before : 0); };
         const int newest = len - 1, last_block = newest / R;
         const int* tab = a.tables + (size_t)b * a.table_stride;
         char* Kh = static_cast<char*>(a.k_pages) + kvh * head_bytes;
@@ -483,23 +495,20 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             st_agent2(part_o_at(slot, h, t + 2), o[2], o[3]);
             if (t == 0) st_agent2(part_ml_at(slot, h), M, L);
         };
-        // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
-        const int w0 = runs.of(head_begin + over), w1 = runs.of(head_begin + per_head - 1), parts = w1 - w0 + 1;
-        const unsigned before = runs.begin(w0) < head_begin ? 1 : 0;
-        auto slot_of = [&](int k) { return 2u * (w0 + k) + (k == 0 ? before : 0); };
         for (int idx = tid; idx < items; idx += 256) {
             const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
-            float M = sh.m[h][0];
+            const f32x4 ms = *reinterpret_cast<const f32x4*>(sh.m[h]), ls = *reinterpret_cast<const f32x4*>(sh.l[h]);
+            f32x4 x[4];
 #pragma unroll
-            for (int w = 1; w < 4; ++w) M = fmaxf(M, sh.m[h][w]);
+            for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&sh.o[w][h][t]);
+            const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
             float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                const float f = sh.m[h][w] > -INFINITY ? __builtin_amdgcn_exp2f(sh.m[h][w] - M) : 0.f;
-                const f32x4 x = *reinterpret_cast<const f32x4*>(&sh.o[w][h][t]);
-                L += sh.l[h][w] * f;
+                const float f = ms[w] > -INFINITY ? __builtin_amdgcn_exp2f(ms[w] - M) : 0.f;
+                L += ls[w] * f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += x[e] * f;
+                for (int e = 0; e < 4; ++e) o[e] += x[w][e] * f;
             }
             if (whole) finish(h, t, o, L); else publish(slot_of(run - w0), h, t, o, M, L);
         }
@@ -588,10 +597,11 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 }
 
 template <typename T, int HD>
-int launch(const PagedAttnArgs& a, int n_cu, hipStream_t s) {
+int launch(PagedAttnArgs a, int n_cu, hipStream_t s) {
     const long long most = (long long)a.B * a.H_kv * paged_head_tiles(a.group) * ((a.max_rows + PagedShape<T, HD>::CH - 1) / PagedShape<T, HD>::CH);
     // as many workgroups as are resident, two per compute unit
     const int n = (int)std::min<long long>(most, std::min(2 * n_cu, kPagedMaxWgs));
+    a.by_runs = Divisor(n);
     if (a.dtype == D3_F32) hipLaunchKernelGGL((attn_paged_kernel<T, HD, float>), dim3(n), dim3(256), 0, s, a);
     else hipLaunchKernelGGL((attn_paged_kernel<T, HD, uint16_t>), dim3(n), dim3(256), 0, s, a);
     return (int)hipGetLastError();

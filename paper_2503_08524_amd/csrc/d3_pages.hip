@@ -123,7 +123,7 @@ extern "C" int d3_pages_reserve(d3_pages* pages, int32_t B, const int32_t* added
     D3_CHECK(check_batch(pages, "d3_pages_reserve", B));
     D3_CHECK(check_tokens("d3_pages_reserve", max_tokens));
     ReserveArgs a{};
-    a.B = B; a.max_pages = pages->desc.max_pages; a.n_pages = pages->desc.n_pages; a.page_rows = pages->desc.page_rows; a.max_tokens = max_tokens;
+    a.B = B; a.max_pages = pages->desc.max_pages; a.n_pages = pages->desc.n_pages; a.page_shift = __builtin_ctz(pages->desc.page_rows); a.max_tokens = max_tokens;
     a.added = added; a.rows_in = rows_in; a.n_free_in = n_free_in;
     a.rows_out = rows_out; a.n_free_out = n_free_out; a.tables = tables; a.free_pages = free_pages;
     a.starts = starts; a.slots = slots; a.positions = positions;
@@ -189,9 +189,10 @@ extern "C" int d3_pages_fill(d3_pages* pages, int32_t n, const int32_t* slots, i
     if (src >= pages->desc.n_layers || (src >= first && src < first + n_layers))
         return fail(D3_ERANGE, "d3_pages_fill: source layer %d must be one of the pool's and outside [%d, %d)", src, first, first + n_layers);
     if (!slots) return fail(D3_EINVAL, "d3_pages_fill: NULL argument");
+    if ((int64_t)n * pages->desc.n_kv_heads > INT32_MAX) return fail(D3_ESHAPE, "d3_pages_fill: %d rows of %d heads are more than one launch counts", n, pages->desc.n_kv_heads);
     const d3_pages_desc& d = pages->desc;
     PagesFillArgs a{};
-    a.n = n; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_rows = d.page_rows; a.first = first; a.n_layers = n_layers; a.src = src < 0 ? -1 : src;
+    a.n = n; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_shift = __builtin_ctz(d.page_rows); a.by_heads = Divisor(d.n_kv_heads); a.first = first; a.n_layers = n_layers; a.src = src < 0 ? -1 : src;
     a.n_slots = pages->n_slots();
     a.slots = slots; a.k_pages = pages->k; a.v_pages = pages->v; a.pool_bytes = pages->pool_bytes();
     const OnDevice on(pages->dev);

@@ -23,7 +23,7 @@ template <> __device__ __forceinline__ f16_t held<f16_t>(float v) { return (f16_
 inline int unit_rows(int kv_dtype) { return 16 / kv_elem_bytes(kv_dtype); }
 
 struct ReserveArgs {
-    int B, max_pages, n_pages, page_rows, max_tokens;
+    int B, max_pages, n_pages, page_shift, max_tokens;
     const int32_t *added, *rows_in, *n_free_in;
     int32_t *rows_out, *n_free_out, *tables, *free_pages, *starts, *slots, *positions;
 };
@@ -43,7 +43,8 @@ struct AppendArgs {
 int launch_pages_append(const AppendArgs& a, int kv_dtype, hipStream_t s);
 
 struct PagesFillArgs {
-    int n, H_kv, hd, page_rows, first, n_layers, src;      // src < 0: zeros
+    int n, H_kv, hd, page_shift, first, n_layers, src;     // src < 0: zeros
+    Divisor by_heads;                      // H_kv
     long long n_slots;
     const int32_t* slots;
     void *k_pages, *v_pages;               // layer 0
@@ -66,6 +67,7 @@ struct PagedAttnArgs {
     SplitForm out_form;
     float *part_o, *part_ml;               // [2 * workgroups][min(group, 16)][hd], [..][2]
     int* tickets;                          // [B][H_kv * tiles], then [2 * workgroups], zero between launches
+    Divisor by_runs;                       // set by launch_attention_paged: its workgroups
 };
 int launch_attention_paged(const PagedAttnArgs& a, int hd, int kv_dtype, int n_cu, hipStream_t s);
 // rows of a workgroup's turn: 4 waves, 16 loads of 16 bytes a lane

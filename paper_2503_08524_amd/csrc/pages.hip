@@ -8,29 +8,43 @@ namespace d3 {
 namespace {
 
 // ---------------- page tables and slot maps ----------------
-// One workgroup: sums over the sequences, each thread a few consecutive ones, then pages and tokens found in those sums by bisection.
-constexpr int kReserveThreads = 1024;
-constexpr int kSeqsPerThread = kPagesMaxSeqs / kReserveThreads;
-
-__device__ __forceinline__ unsigned long long shfl_up64(unsigned long long v, int o) {
-    const unsigned lo = __shfl_up((unsigned)v, o, 64), hi = __shfl_up((unsigned)(v >> 32), o, 64);
+// One workgroup: sums over the sequences (a wave's by row shifts, no LDS; the waves' through LDS), then pages and tokens found in those sums by bisection.  A chain of round trips
+// bounds it: requests in, sums, pages of the stack, tables, slots.
+__device__ __forceinline__ unsigned long long shifted64(unsigned long long v, int which) {
+    unsigned lo, hi;
+#define D3_SHIFT(ctrl, rows) lo = __builtin_amdgcn_update_dpp(0, (unsigned)v, ctrl, rows, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (unsigned)(v >> 32), ctrl, rows, 0xf, false)
+    switch (which) {
+        case 0: D3_SHIFT(0x111, 0xf); break;
+        case 1: D3_SHIFT(0x112, 0xf); break;
+        case 2: D3_SHIFT(0x114, 0xf); break;
+        case 3: D3_SHIFT(0x118, 0xf); break;
+        case 4: D3_SHIFT(0x142, 0xa); break;
+        default: D3_SHIFT(0x143, 0xc);
+    }
+#undef D3_SHIFT
     return (unsigned long long)hi << 32 | lo;
 }
-// Sum over the threads before this one, and over all; `red`: a word per wave, free again behind the next barrier but one.
+// Sum over the threads before this one, and over all; `red`: a word per wave.
+template <int THREADS>
 __device__ __forceinline__ unsigned long long scan_block(unsigned long long v, unsigned long long* red, unsigned long long* all) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int WAVES = THREADS / 64;
     unsigned long long s = v;
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        const unsigned long long below = shfl_up64(s, o);
-        if (lane >= o) s += below;
+    for (int k = 0; k < 6; ++k) s += shifted64(s, k);
+    const unsigned long long last = (unsigned long long)__builtin_amdgcn_readlane((unsigned)(s >> 32), 63) << 32 | (unsigned)__builtin_amdgcn_readlane((unsigned)s, 63);
+    if constexpr (WAVES == 1) {
+        *all = last;
+        return s - v;
     }
-    if (lane == 63) red[wave] = s;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 63) red[wave] = s;
     __syncthreads();
     unsigned long long before = 0, sum = 0;
-    for (int w = 0; w < kReserveThreads / 64; ++w) {
-        if (w < wave) before += red[w];
-        sum += red[w];
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const unsigned long long x = red[w];
+        if (w < wave) before += x;
+        sum += x;
     }
     *all = sum;
     return before + s - v;
@@ -51,59 +65,66 @@ __device__ __forceinline__ void write_token(const ReserveArgs& a, const int* sta
     if (t < starts[a.B]) {
         const int b = last_at_most(starts, a.B, t);                 // sequences that got nothing share their start with the next one
         p = a.rows_out[b] - starts[b + 1] + t;
-        const int page = a.tables[(size_t)b * a.max_pages + p / a.page_rows];
-        if ((unsigned)page < (unsigned)a.n_pages) slot = page * a.page_rows + p % a.page_rows;
+        const int page = a.tables[(size_t)b * a.max_pages + (p >> a.page_shift)];
+        if ((unsigned)page < (unsigned)a.n_pages) slot = (page << a.page_shift) + (p & ((1 << a.page_shift) - 1));
     }
     a.slots[t] = slot;
     if (a.positions) a.positions[t] = p;
 }
 
-__global__ __launch_bounds__(kReserveThreads) void pages_reserve_kernel(ReserveArgs a, int write_tokens) {
-    __shared__ int starts[kPagesMaxSeqs + 1], page_at[kPagesMaxSeqs + 1], back_at[kPagesMaxSeqs + 1], page_first[kPagesMaxSeqs];
-    __shared__ unsigned long long red[3][kReserveThreads / 64];
-    const int tid = threadIdx.x, b0 = tid * kSeqsPerThread, cap = a.max_pages * a.page_rows;
-    auto pages_of = [&](int rows) { return (int)(((unsigned)rows + a.page_rows - 1) / a.page_rows); };
-    int rows[kSeqsPerThread], need[kSeqsPerThread], back[kSeqsPerThread];
-    long long asked[kSeqsPerThread];
+// THREADS * EACH sequences at most, EACH consecutive ones a thread
+template <int THREADS, int EACH>
+__global__ __launch_bounds__(THREADS) void pages_reserve_kernel(ReserveArgs a, int write_tokens) {
+    constexpr int MOST = THREADS * EACH;
+    __shared__ int starts[MOST + 1], page_at[MOST + 1], back_at[MOST + 1], page_first[MOST];
+    __shared__ unsigned long long red[3][THREADS / 64];
+    const int tid = threadIdx.x, b0 = tid * EACH, cap = a.max_pages << a.page_shift;
+    auto pages_of = [&](int rows) { return (int)(((unsigned)rows + (1u << a.page_shift) - 1) >> a.page_shift); };
+    int rows[EACH], need[EACH], back[EACH], add[EACH];
+    long long asked[EACH];
     unsigned long long mine = 0, all;
+    const int free_in = a.n_free_in[0];
 #pragma unroll
-    for (int j = 0; j < kSeqsPerThread; ++j) {
+    for (int j = 0; j < EACH; ++j) {
         const int b = b0 + j;
-        const int add = b < a.B ? a.added[b] : 0;
-        rows[j] = b < a.B ? min(max(a.rows_in[b], 0), cap) : 0;
-        back[j] = add < 0 ? pages_of(rows[j]) : 0;
-        if (add < 0) rows[j] = 0;
-        asked[j] = add > 0 && (long long)rows[j] + add <= cap ? add : 0;
+        add[j] = b < a.B ? a.added[b] : 0;
+        rows[j] = b < a.B ? a.rows_in[b] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        rows[j] = min(max(rows[j], 0), cap);
+        back[j] = add[j] < 0 ? pages_of(rows[j]) : 0;
+        if (add[j] < 0) rows[j] = 0;
+        asked[j] = add[j] > 0 && (long long)rows[j] + add[j] <= cap ? add[j] : 0;
         mine += asked[j];
     }
     // what of it fits max_tokens, the pages that needs, and the pages that come back: two sums in one word, neither passes 2^31
-    unsigned long long before = scan_block(mine, red[0], &all), both = 0;
+    unsigned long long before = scan_block<THREADS>(mine, red[0], &all), both = 0;
 #pragma unroll
-    for (int j = 0; j < kSeqsPerThread; ++j) {
+    for (int j = 0; j < EACH; ++j) {
         before += asked[j];
         if (before > (unsigned long long)a.max_tokens) asked[j] = 0;
         need[j] = pages_of(rows[j] + (int)asked[j]) - pages_of(rows[j]);
         both += (unsigned long long)need[j] << 32 | (unsigned)back[j];
     }
-    before = scan_block(both, red[1], &all);
+    before = scan_block<THREADS>(both, red[1], &all);
     const long long wanted = all >> 32, returned = (unsigned)all;
-    const int n_free = min(max(a.n_free_in[0], 0), a.n_pages), avail = (int)min((long long)n_free + returned, (long long)a.n_pages);
+    const int n_free = min(max(free_in, 0), a.n_pages), avail = (int)min((long long)n_free + returned, (long long)a.n_pages);
     int need_before = (int)(before >> 32), back_before = (int)(unsigned)before;
     both = 0;
-    int granted[kSeqsPerThread], first[kSeqsPerThread];
+    int granted[EACH];
 #pragma unroll
-    for (int j = 0; j < kSeqsPerThread; ++j) {
-        first[j] = need_before;                                     // a refusal for pages refuses all behind it that need some: the sum is that of granted ones
-        granted[j] = need[j] == 0 || need_before + need[j] <= avail ? (int)asked[j] : 0;
+    for (int j = 0; j < EACH; ++j) {
+        granted[j] = need[j] == 0 || need_before + need[j] <= avail ? (int)asked[j] : 0;       // a refusal for pages refuses all behind it that need some
         need_before += need[j];
         if (granted[j] == 0) need[j] = 0;
         both += (unsigned long long)need[j] << 32 | (unsigned)granted[j];
     }
-    before = scan_block(both, red[2], &all);
+    before = scan_block<THREADS>(both, red[2], &all);
     const int taken = (int)(all >> 32), tokens = (int)(unsigned)all;
     int start = (int)(unsigned)before, page = (int)(before >> 32);
 #pragma unroll
-    for (int j = 0; j < kSeqsPerThread; ++j) {
+    for (int j = 0; j < EACH; ++j) {
         const int b = b0 + j;
         if (b >= a.B) break;
         starts[b] = start; page_at[b] = page; back_at[b] = back_before;
@@ -121,18 +142,20 @@ __global__ __launch_bounds__(kReserveThreads) void pages_reserve_kernel(ReserveA
         a.n_free_out[0] = avail - taken;
         a.n_free_out[1] = (int)max(wanted - avail, 0ll);
     }
-    for (int x = tid; x < avail - n_free; x += kReserveThreads) {
-        const int b = last_at_most(back_at, a.B, x);
-        a.free_pages[n_free + x] = a.tables[(size_t)b * a.max_pages + x - back_at[b]];
+    if (avail > n_free) {
+        for (int x = tid; x < avail - n_free; x += THREADS) {
+            const int b = last_at_most(back_at, a.B, x);
+            a.free_pages[n_free + x] = a.tables[(size_t)b * a.max_pages + x - back_at[b]];
+        }
+        __syncthreads();
     }
-    __syncthreads();
-    for (int x = tid; x < taken; x += kReserveThreads) {
+    for (int x = tid; x < taken; x += THREADS) {
         const int b = last_at_most(page_at, a.B, x);
         a.tables[(size_t)b * a.max_pages + page_first[b] + x - page_at[b]] = a.free_pages[avail - 1 - x];
     }
     if (!write_tokens) return;
     __syncthreads();
-    for (int t = tid; t < a.max_tokens; t += kReserveThreads) write_token(a, starts, t);
+    for (int t = tid; t < a.max_tokens; t += THREADS) write_token(a, starts, t);
 }
 
 // the tokens alone, behind the kernel above
@@ -140,7 +163,8 @@ __global__ __launch_bounds__(256) void pages_slots_kernel(ReserveArgs a) {
     __shared__ int starts[kPagesMaxSeqs + 1];
     for (int b = threadIdx.x; b <= a.B; b += 256) starts[b] = a.starts[b];
     __syncthreads();
-    for (int t = blockIdx.x * 1024 + threadIdx.x; t < min(a.max_tokens, ((int)blockIdx.x + 1) * 1024); t += 256) write_token(a, starts, t);
+    const int t = blockIdx.x * 256 + threadIdx.x;
+    if (t < a.max_tokens) write_token(a, starts, t);
 }
 
 // ---------------- rows into pages ----------------
@@ -267,32 +291,43 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
 }
 
 // ---------------- missing-state fill on pages ----------------
-// A thread has one piece of a row (16 bytes of the key, or one element of the value) of one (token, KV head), reads it once from the source block
-// and writes it into a few of the dropped ones (grid.y).
-template <typename T>
+// A wave has one (token, KV head): 16 bytes of the key in the first lanes, one or two elements of the value in each, read once from the source block
+// and written into a few of the dropped ones (grid.y).
+template <typename T, int HD>
 __global__ __launch_bounds__(256) void pages_fill_kernel(PagesFillArgs a, int layers_each) {
-    constexpr int R = 16 / sizeof(T);
-    const int k_pieces = a.hd / R, pieces = k_pieces + a.hd;
-    const long long x = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int piece = (int)(x % pieces), head = (int)(x / pieces % a.H_kv);
-    const long long t = x / pieces / a.H_kv;
-    if (t >= a.n) return;
-    const int slot = a.slots[t];
+    constexpr int R = 16 / sizeof(T), DL = HD / 64;
+    const int lane = threadIdx.x & 63, unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (unit >= a.n * a.H_kv) return;
+    const int t = a.by_heads.of(unit), head = unit - t * a.H_kv, slot = a.slots[t];
     if (slot < 0 || slot >= a.n_slots) return;
-    const int row = slot % a.page_rows;
-    const size_t base = ((size_t)(slot / a.page_rows) * a.H_kv + head) * a.page_rows * a.hd;
+    const int row = slot & ((1 << a.page_shift) - 1);
+    const size_t base = (((size_t)(slot >> a.page_shift) * a.H_kv + head) << a.page_shift) * HD;
     const int l0 = a.first + blockIdx.y * layers_each, l1 = min(l0 + layers_each, a.first + a.n_layers);
-    if (piece < k_pieces) {
-        char* at = static_cast<char*>(a.k_pages) + (base + (size_t)row * a.hd + piece * R) * sizeof(T);
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (a.src >= 0) v = *reinterpret_cast<const uint4*>(at + a.src * a.pool_bytes);
-        for (int l = l0; l < l1; ++l) *reinterpret_cast<uint4*>(at + l * a.pool_bytes) = v;
-    } else {
-        char* at = static_cast<char*>(a.v_pages) + (base + (size_t)(row / R * a.hd + piece - k_pieces) * R + row % R) * sizeof(T);
-        T v{};
-        if (a.src >= 0) v = *reinterpret_cast<const T*>(at + a.src * a.pool_bytes);
-        for (int l = l0; l < l1; ++l) *reinterpret_cast<T*>(at + l * a.pool_bytes) = v;
+    const bool has_key = lane < HD / R;
+    char* k_at = static_cast<char*>(a.k_pages) + (base + (size_t)row * HD + (has_key ? lane : 0) * R) * sizeof(T);
+    char* v_at = static_cast<char*>(a.v_pages) + (base + (size_t)(row / R * HD + lane * DL) * R + row % R) * sizeof(T);
+    uint4 kv = make_uint4(0, 0, 0, 0);
+    T vv[DL] = {};
+    if (a.src >= 0) {
+        kv = *reinterpret_cast<const uint4*>(k_at + a.src * a.pool_bytes);
+#pragma unroll
+        for (int d = 0; d < DL; ++d) vv[d] = *reinterpret_cast<const T*>(v_at + a.src * a.pool_bytes + d * 16);
     }
+    for (int l = l0; l < l1; ++l) {
+        if (has_key) *reinterpret_cast<uint4*>(k_at + l * a.pool_bytes) = kv;
+#pragma unroll
+        for (int d = 0; d < DL; ++d) *reinterpret_cast<T*>(v_at + l * a.pool_bytes + d * 16) = vv[d];
+    }
+}
+
+template <typename T>
+int launch_fill(const PagesFillArgs& a, hipStream_t s) {
+    // enough waves for the chip's latency first, then as many blocks to a wave as can be
+    const int units = a.n * a.H_kv, each = units >= 4096 ? a.n_layers : units >= 512 ? 8 : 4;
+    const dim3 grid((units + 3) / 4, (a.n_layers + each - 1) / each);
+    if (a.hd == 64) hipLaunchKernelGGL((pages_fill_kernel<T, 64>), grid, dim3(256), 0, s, a, each);
+    else hipLaunchKernelGGL((pages_fill_kernel<T, 128>), grid, dim3(256), 0, s, a, each);
+    return (int)hipGetLastError();
 }
 
 template <typename S, typename T>
@@ -310,12 +345,14 @@ int launch_append_to(const AppendArgs& a, hipStream_t s) {
 }  // namespace
 
 int launch_pages_reserve(const ReserveArgs& a, hipStream_t s) {
-    // few tokens (a step's): by the same workgroup; many: by a launch of their own over the chip
-    const bool few = a.max_tokens <= 4 * kReserveThreads;
-    hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kReserveThreads), 0, s, a, few ? 1 : 0);
+    // Few tokens (a step's): by the same workgroup; many: by a launch of their own over the chip.
+    const bool few = a.max_tokens <= (a.B <= 64 ? 512 : 4096);
+    if (a.B <= 64) hipLaunchKernelGGL((pages_reserve_kernel<64, 1>), dim3(1), dim3(64), 0, s, a, few ? 1 : 0);
+    else if (a.B <= 1024) hipLaunchKernelGGL((pages_reserve_kernel<1024, 1>), dim3(1), dim3(1024), 0, s, a, few ? 1 : 0);
+    else hipLaunchKernelGGL((pages_reserve_kernel<1024, kPagesMaxSeqs / 1024>), dim3(1), dim3(1024), 0, s, a, few ? 1 : 0);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || few) return (int)e;
-    hipLaunchKernelGGL(pages_slots_kernel, dim3((unsigned)((a.max_tokens + 1023ll) / 1024)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(pages_slots_kernel, dim3((a.max_tokens + 255) / 256), dim3(256), 0, s, a);
     return (int)hipGetLastError();
 }
 
@@ -324,12 +361,7 @@ int launch_pages_append(const AppendArgs& a, int kv_dtype, hipStream_t s) {
 }
 
 int launch_pages_fill(const PagesFillArgs& a, int kv_dtype, hipStream_t s) {
-    const long long threads = (long long)a.n * a.H_kv * (a.hd / unit_rows(kv_dtype) + a.hd);
-    const int each = 8;
-    const dim3 grid((unsigned)((threads + 255) / 256), (a.n_layers + each - 1) / each);
-    if (kv_dtype == D3_F32) hipLaunchKernelGGL(pages_fill_kernel<float>, grid, dim3(256), 0, s, a, each);
-    else hipLaunchKernelGGL(pages_fill_kernel<f16_t>, grid, dim3(256), 0, s, a, each);
-    return (int)hipGetLastError();
+    return kv_dtype == D3_F32 ? launch_fill<float>(a, s) : launch_fill<f16_t>(a, s);
 }
 
 }  // namespace d3
