@@ -176,30 +176,27 @@ __global__ __launch_bounds__(256) void pages_slots_kernel(ReserveArgs a) {
 }
 
 // ---------------- rows into pages ----------------
-template <typename S> __device__ __forceinline__ void load8(const S* p, float (&y)[8]);
-template <> __device__ __forceinline__ void load8<float>(const float* p, float (&y)[8]) {
-    const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-    y[0] = a.x; y[1] = a.y; y[2] = a.z; y[3] = a.w; y[4] = b.x; y[5] = b.y; y[6] = b.z; y[7] = b.w;
-}
-template <> __device__ __forceinline__ void load8<bf16_t>(const bf16_t* p, float (&y)[8]) {
-    const uint4 v = *reinterpret_cast<const uint4*>(p);
-    y[0] = bf16_lo(v.x); y[1] = bf16_hi(v.x); y[2] = bf16_lo(v.y); y[3] = bf16_hi(v.y);
-    y[4] = bf16_lo(v.z); y[5] = bf16_hi(v.z); y[6] = bf16_lo(v.w); y[7] = bf16_hi(v.w);
-}
-template <> __device__ __forceinline__ void load8<f16_t>(const f16_t* p, float (&y)[8]) {
-    typedef _Float16 half8 __attribute__((ext_vector_type(8)));
-    const half8 v = *reinterpret_cast<const half8*>(p);
+// E adjacent elements, 16 bytes of S or T at a time
+template <int E, typename S> __device__ __forceinline__ void load_many(const S* p, float (&y)[E]) {
+    constexpr int N = 16 / sizeof(S);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = (float)v[e];
-}
-template <typename T> __device__ __forceinline__ void store8(T* p, const float (&y)[8]) {
-    alignas(16) T t[8];
+    for (int e = 0; e < E; e += N) {
+        alignas(16) S t[N];
+        *reinterpret_cast<u32x4*>(t) = *reinterpret_cast<const u32x4*>(p + e);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) t[e] = held<T>(y[e]);
-#pragma unroll
-    for (int e = 0; e < 8; e += 16 / sizeof(T)) *reinterpret_cast<uint4*>(p + e) = *reinterpret_cast<const uint4*>(t + e);
+        for (int j = 0; j < N; ++j) { if constexpr (std::is_same<S, bf16_t>::value) y[e + j] = bf16_to_f32(t[j]); else y[e + j] = (float)t[j]; }
+    }
 }
-
+template <int E, typename T> __device__ __forceinline__ void store_many(T* p, const float (&y)[E]) {
+    alignas(16) T t[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) t[e] = held<T>(y[e]);
+    if constexpr (E * sizeof(T) == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(t);
+    else {
+#pragma unroll
+        for (int e = 0; e < E; e += 16 / sizeof(T)) *reinterpret_cast<uint4*>(p + e) = *reinterpret_cast<const uint4*>(t + e);
+    }
+}
 // N = 1 or 2 adjacent elements
 template <int N, typename S> __device__ __forceinline__ void load_few(const S* p, float (&y)[N]) {
     if constexpr (N == 2 && sizeof(S) == 4) { const float2 v = *reinterpret_cast<const float2*>(p); y[0] = v.x; y[1] = v.y; }
@@ -214,7 +211,7 @@ template <int N, typename S> __device__ __forceinline__ void load_few(const S* p
 }
 
 // grid: (32 tokens, KV head, layer and half: keys or values); a wave has 8 tokens.
-// A key is a row of its page: eight dims of the lower half and their partners per thread.
+// A key is a row of its page: 16 bytes of the lower half and their partners per thread.
 // Of a value's dims R rows lie side by side in 16 bytes.  A lane has one or two dims: where a token is row 0 of a unit of R rows that follow each other in
 // `slots`, its wave loads those R rows (whole lines each) and writes the unit's 16 bytes per dim, for all of them, also those of the next wave's tokens;
 // only rows of units that the call does not fill are written element by element.  What each token is, is one wave's business: bits of a mask.
@@ -236,29 +233,30 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
         return slot < a.n_slots ? slot : -1;
     };
     if (!values) {
-        constexpr int PER = HD / 16;                               // threads of a token
-        for (int x = tid; x < kAppendTokens * PER; x += 256) {
-            const int t = blockIdx.x * kAppendTokens + x / PER, j = x % PER * 8, slot = slot_at(t);
+        constexpr int E = 16 / sizeof(S), PER = HD / (2 * E);      // threads of a token, each with one load of either half
+#pragma unroll
+        for (int x0 = 0; x0 < kAppendTokens * PER; x0 += 256) {
+            const int x = x0 + tid, t = blockIdx.x * kAppendTokens + x / PER, j = x % PER * E, slot = x < kAppendTokens * PER ? slot_at(t) : -1;
             if (slot < 0) continue;
-            float lo[8], hi[8];
+            float lo[E], hi[E];
             const S* row = src + t * a.token_stride;
-            load8<S>(row + j, lo);
-            load8<S>(row + j + HD / 2, hi);
+            load_many<E, S>(row + j, lo);
+            load_many<E, S>(row + j + HD / 2, hi);
             if (a.rope_cs) {
-                float cs[16];
                 const float2* c = a.rope_cs + (size_t)t * (HD / 2) + j;
+                float2 cs[E];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) { cs[2 * e] = c[e].x; cs[2 * e + 1] = c[e].y; }
+                for (int e = 0; e < E; ++e) cs[e] = c[e];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
+                for (int e = 0; e < E; ++e) {
                     const float x0 = lo[e], x1 = hi[e];
-                    lo[e] = x0 * cs[2 * e] - x1 * cs[2 * e + 1];
-                    hi[e] = x1 * cs[2 * e] + x0 * cs[2 * e + 1];
+                    lo[e] = x0 * cs[e].x - x1 * cs[e].y;
+                    hi[e] = x1 * cs[e].x + x0 * cs[e].y;
                 }
             }
             T* to = pool_at(a.k_pages, slot) + (slot & row_mask) * HD + j;
-            store8<T>(to, lo);
-            store8<T>(to + HD / 2, hi);
+            store_many<E, T>(to, lo);
+            store_many<E, T>(to + HD / 2, hi);
         }
         return;
     }
