@@ -253,7 +253,7 @@ typedef struct d3_pages d3_pages;
 size_t d3_pages_workspace_size(const d3_pages_desc *desc);
 
 /* Handle on caller-owned pools and workspace (256-byte aligned, d3_pages_workspace_size bytes; pools 16-byte aligned), on the current
- * device, which the calls below make current for themselves.  Waits for the device once (it clears the counters). */
+ * device, which the calls below make current for themselves.  Clears the counters on the null stream and waits for it. */
 int d3_pages_create(d3_pages **out, const d3_pages_desc *desc, void *k_pages, void *v_pages, void *workspace, size_t workspace_bytes);
 int d3_pages_destroy(d3_pages *pages);
 

@@ -346,7 +346,9 @@ class PagedCache:
             self.tables = buffer("tables", tables, (max_batch, max_pages), torch.int32, none)
             self.rows = buffer("rows", rows, (max_batch,), torch.int32, torch.zeros)
             self.free_pages = buffer("free_pages", free_pages, (n_pages,), torch.int32, lambda dims, **kw: torch.arange(n_pages - 1, -1, -1, **kw))
-            self.n_free = buffer("n_free", n_free, (2,), torch.int32, lambda dims, **kw: torch.tensor([n_pages, 0], **kw))
+            self.n_free = buffer("n_free", n_free, (2,), torch.int32, torch.zeros)
+            if n_free is None:
+                self.n_free[:1].fill_(n_pages)
             self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
             handle = C.c_void_p()
             _check(self.lib.d3_pages_create(C.byref(handle), C.byref(desc), self.k_pages.data_ptr(), self.v_pages.data_ptr(),

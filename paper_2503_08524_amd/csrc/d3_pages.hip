@@ -1,6 +1,7 @@
 // C ABI of the paged key-value cache: handle and argument checks.  All device memory is the caller's.
-#include <new>
+#include <atomic>
 #include <cstring>
+#include <new>
 
 #include "d3_error.h"
 #include "pages.h"
@@ -76,6 +77,23 @@ int check_dtype(const char* who, int32_t dtype) {
         if (rc_ != D3_OK) return rc_;   \
     } while (0)
 
+namespace {
+// Compute units of a gfx950 device, asked once per device (the properties take longer than the rest of d3_pages_create).
+int device_cus(int dev, int* n_cu) {
+    constexpr int kMaxDevices = 64;
+    static std::atomic<int> known[kMaxDevices];
+    if (dev < 0 || dev >= kMaxDevices) return fail(D3_EDEVICE, "d3_pages_create: device index %d is outside [0, %d)", dev, kMaxDevices);
+    *n_cu = known[dev].load(std::memory_order_relaxed);
+    if (*n_cu > 0) return D3_OK;
+    hipDeviceProp_t prop;
+    D3_HIP(hipGetDeviceProperties(&prop, dev));
+    if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return fail(D3_EDEVICE, "d3_pages_create: built for gfx950, device is %s", prop.gcnArchName);
+    *n_cu = prop.multiProcessorCount;
+    known[dev].store(*n_cu, std::memory_order_relaxed);
+    return D3_OK;
+}
+}  // namespace
+
 extern "C" size_t d3_pages_workspace_size(const d3_pages_desc* desc) {
     if (check_desc(desc) != D3_OK) return 0;
     size_t ml, tickets;
@@ -92,19 +110,17 @@ extern "C" int d3_pages_create(d3_pages** out, const d3_pages_desc* desc, void* 
     size_t part_ml, tickets;
     const size_t need = layout(*desc, &part_ml, &tickets);
     if (workspace_bytes < need) return fail(D3_EINVAL, "d3_pages_create: workspace has %zu bytes, %zu needed", workspace_bytes, need);
-    int dev = 0;
-    hipDeviceProp_t prop;
+    int dev = 0, n_cu = 0;
     D3_HIP(hipGetDevice(&dev));
-    D3_HIP(hipGetDeviceProperties(&prop, dev));
-    if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return fail(D3_EDEVICE, "d3_pages_create: built for gfx950, device is %s", prop.gcnArchName);
+    D3_CHECK(device_cus(dev, &n_cu));
     d3_pages* p = new (std::nothrow) d3_pages();
     if (!p) return fail(D3_EINVAL, "d3_pages_create: out of host memory");
     p->desc = *desc;
     p->k = static_cast<char*>(k_pages); p->v = static_cast<char*>(v_pages); p->ws = static_cast<char*>(workspace);
-    p->dev = dev; p->n_cu = prop.multiProcessorCount;
+    p->dev = dev; p->n_cu = n_cu;
     p->part_ml = part_ml; p->tickets = tickets;
     hipError_t e = hipMemset(p->ws + tickets, 0, need - tickets);              // arrival counters start at 0
-    if (e == hipSuccess) e = hipDeviceSynchronize();                          // calls may come on any stream
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);                   // calls may come on any stream
     if (e != hipSuccess) { delete p; return fail(D3_EDEVICE, "d3_pages_create: hipMemset failed: %s", hipGetErrorString(e)); }
     *out = p;
     return D3_OK;

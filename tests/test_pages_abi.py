@@ -26,9 +26,9 @@ def size(lib, **change):
     return lib.d3_pages_workspace_size(C.byref(desc(**change)))
 
 
-def test_workspace_holds_two_partials_a_workgroup_and_a_counter_per_sequence_and_heads(lib):
+def test_workspace_holds_two_partials_and_counters_a_workgroup_and_a_counter_per_sequence_and_heads(lib):
     n = size(lib)
-    assert n % 256 == 0 and 2 * 1024 * 4 * 130 * 4 <= n <= 2 * 1024 * 4 * 130 * 4 + 1024
+    assert n % 256 == 0 and 2 * 1024 * (4 * 130 * 4 + 4) <= n <= 2 * 1024 * (4 * 130 * 4 + 4) + 1024
     assert size(lib, n_heads=64, n_kv_heads=2) == size(lib, n_heads=32, n_kv_heads=2)      # 32 heads of a KV head are taken 16 at a time
     assert size(lib, max_batch=4096) - n == (4096 - 4) * 2 * 4 // 256 * 256
     assert size(lib, n_pages=100000) == n
