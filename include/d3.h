@@ -279,7 +279,7 @@ int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n,
 
 /* Attention of one token per sequence over its pages: out[b][h] = softmax(scale * q[b][h] . K^T) V over rows [0, rows[b]) of sequence b; 0 where it has no row.
  * q, out: dev [B][n_heads][head_dim] of `dtype`, sequence b at b * q_stride, b * out_stride.  k_new, v_new: dev [B][H_kv][head_dim] of `dtype` at b * kv_stride, or both NULL.
- * Given, they are row rows[b] - 1, which the call also writes to its page; else that row is there already.  rope_cs: dev float [B][head_dim / 2][2]: q and
+ * Given, they are row rows[b] - 1, which the call also writes to its page (which no other sequence of the call may list); else that row is there already.  rope_cs: dev float [B][head_dim / 2][2]: q and
  * k_new turn by it; NULL: neither does.  q, k_new, v_new, rope_cs 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
  * Keys and values are used as the pool holds them; sums and softmax in 32 bits. */
 int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,

@@ -317,6 +317,8 @@ class PagedCache:
         self.lib = load_library()
         self.handle = None
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim = n_layers, n_heads, n_kv_heads, head_dim
         self.n_pages, self.page_rows, self.max_batch, self.max_pages, self.kv_dtype = n_pages, page_rows, max_batch, max_pages, kv_dtype
         kinds = {"f32": D3_F32, "bf16": D3_BF16, "f16": D3_F16}
@@ -328,7 +330,7 @@ class PagedCache:
             raise D3Error(-2, self.lib.d3_last_error().decode())
         self._kinds = {torch.float32: D3_F32, torch.bfloat16: D3_BF16, torch.float16: D3_F16}
         self._int32, self._float32 = torch.int32, torch.float32
-        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        self._index = self.device.index
         # the current stream's handle without the object around it (2 us a call), where torch offers that
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
         tdt = {"f32": torch.float32, "f16": torch.float16}[kv_dtype]

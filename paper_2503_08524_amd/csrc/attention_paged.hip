@@ -98,6 +98,19 @@ __device__ __forceinline__ void store_act4(void* p, long long at, int dtype, con
     else { h[0] = (uint16_t)w.x; h[1] = (uint16_t)(w.x >> 16); h[2] = (uint16_t)w.y; h[3] = (uint16_t)(w.y >> 16); }
 }
 
+// x = hi + lo
+__device__ __forceinline__ void split_half8(const float (&x)[8], half8& hi, half8& lo) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const half2 h = __builtin_convertvector((f32x2{x[e], x[e + 1]}), half2);
+        const half2 l = __builtin_convertvector((f32x2{x[e] - (float)h[0], x[e + 1] - (float)h[1]}), half2);
+        hi[e] = h[0]; hi[e + 1] = h[1];
+        lo[e] = l[0]; lo[e + 1] = l[1];
+    }
+}
+
 // st_agent, ld_agent of two adjacent floats
 __device__ __forceinline__ void st_agent2(float* p, float x, float y) {
     __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -218,8 +231,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
         const int* tab = a.tables + (size_t)b * a.table_stride;
         char* Kh = static_cast<char*>(a.k_pages) + kvh * head_bytes;
         char* Vh = static_cast<char*>(a.v_pages) + kvh * head_bytes;
-        const int rend = min(c1 * P::CH, len);
-        int r = c0 * P::CH + wave * P::TR;                          // first row of this wave's turn
+        // This wave's turns: rows first, first + CH, ... last, in a circle that begins at another place in every workgroup.  (Sequences whose pages lie a power of two apart, 64 pages
+        // each, are at the same place of their memory channels in every row; workgroups that walk them in step meet there.)
+        const int first = c0 * P::CH + wave * P::TR, turns = c1 - c0 - ((c1 - 1) * P::CH + wave * P::TR >= len ? 1 : 0), last = first + (turns - 1) * P::CH;
+        int r = first;
+        if (turns >= 4) r += (run - small_quotient(run, turns) * turns) * P::CH;       // (a few turns do not meet for long)
+        auto after = [&](int row) { return row == last ? first : row + P::CH; };
 
         uint4 kr[U][KT][NK], vr[U][ND];
         // pages of the blocks of R rows that a lane loads of K and of V; blocks past the last are read as the last
@@ -257,7 +274,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
         f32x4 acc[ND];
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (r < rend) {
+        if (turns > 0) {
             A nk[2], nv[2];                                         // dims `lane` and lane + HD / 2 of the newest row
             float2 ncs = {1.f, 0.f};
             if (fresh) {
@@ -271,7 +288,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             }
             int pk[U], pv[U], pk1[U], pv1[U];
             load_pages(r, pk, pv);
-            load_pages(r + P::CH, pk1, pv1);
+            load_pages(after(r), pk1, pv1);
             float qf[NK][QE];
             ActVec<QE, A> qa[NK];
 #pragma unroll
@@ -283,6 +300,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                 for (int k = 0; k < NK / 2; ++k) cs[k].load(reinterpret_cast<const float*>(a.rope_cs + (size_t)b * (HD / 2) + k * 4 * QE + g * QE));
             }
             const int new_page = tab[last_block >> block_shift];
+            uint4 unit[2];                                          // the values of dims `lane` and lane + HD / 2 beside the newest row's: R rows share 16 bytes
+            char* const unit_at = Vh + (size_t)(present(new_page) ? new_page : 0) * page_bytes + ((last_block & block_mask) * HD + lane % (HD / 2)) * 16;
+            if (fresh) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) unit[e] = *reinterpret_cast<const uint4*>(unit_at + e * (HD * 8));
+            }
             __builtin_amdgcn_sched_barrier(0);
             issue_k(r, pk);
             issue_v(r, pv);
@@ -298,7 +321,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         sh.new_k[d] = kt; sh.new_v[d] = vt;
                         if (h0 == 0 && present(new_page)) {
                             reinterpret_cast<T*>(Kh + new_page * page_bytes)[(newest & ((1 << a.page_shift) - 1)) * HD + d] = kt;
-                            reinterpret_cast<T*>(Vh + new_page * page_bytes)[((last_block & block_mask) * HD + d) * R + newest % R] = vt;
+                            T rows[R];
+                            __builtin_memcpy(rows, &unit[e], 16);
+#pragma unroll
+                            for (int j = 0; j < R; ++j) if (newest % R == j) rows[j] = vt;
+                            // whole lines (two bytes of every 16 would be 5 us of 190 with 1024 of these)
+                            __builtin_memcpy(unit_at + e * (HD * 8), rows, 16);
                         }
                     }
                 }
@@ -320,7 +348,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             }
             // q as fp16 halves hi + lo, scaled by a power of two that puts its largest element at 2^14: 22 bits of it
             float mul = a.scale * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
-            half8 qh[NK], ql[NK];
+            // In LDS from here on (where this wave puts its outputs in the end): in registers it would leave too few for the rows in flight.
+            uint4* const q_lds = reinterpret_cast<uint4*>(sh.o[wave]) + lane;
             if constexpr (P::ES == 2) {
                 float top = 0.f;
 #pragma unroll
@@ -328,26 +357,33 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 #pragma unroll
                     for (int e = 0; e < QE; ++e) top = fmaxf(top, fabsf(qf[k][e]));
                 top = reduce_halves(reduce_row_pairs(top, MaxOp()), MaxOp());
-                const int ex = top > 0.f && top < INFINITY ? 14 - ilogbf(top) : 0;
+                const int ex = 15 - __builtin_amdgcn_frexp_expf(top);
 #pragma unroll
-                for (int k = 0; k < NK; ++k)
+                for (int k = 0; k < NK; ++k) {
+                    half8 hi, lo;
 #pragma unroll
-                    for (int e = 0; e < QE; ++e) {
-                        const float v = ldexpf(qf[k][e], ex);
-                        qh[k][e] = (_Float16)v;
-                        ql[k][e] = (_Float16)(v - (float)qh[k][e]);
-                    }
-                mul = ldexpf(mul, -ex);
+                    for (int e = 0; e < QE; ++e) qf[k][e] = __builtin_ldexpf(qf[k][e], ex);
+                    split_half8(qf[k], hi, lo);
+                    q_lds[(2 * k) * 64] = __builtin_bit_cast(uint4, hi);
+                    q_lds[(2 * k + 1) * 64] = __builtin_bit_cast(uint4, lo);
+                }
+                mul = __builtin_ldexpf(mul, -ex);
+            } else {
+#pragma unroll
+                for (int k = 0; k < NK; ++k) __builtin_memcpy(&q_lds[k * 64], qf[k], 16);
             }
+            static_assert((P::ES == 2 ? 2 : 1) * NK * 64 * 16 <= sizeof(sh.o[0]), "");
 
             auto turn = [&](auto more_) {
-                constexpr bool MORE = decltype(more_)::value;
-                const bool tail = !MORE && r + P::TR >= len;        // holds the newest row, or rows past it
+                constexpr bool MORE = decltype(more_)::value;       // another turn follows
+                const int next_r = after(r);
+                const bool tail = r + P::TR >= len;                 // holds the newest row, or rows past it
+                const bool with_new = fresh && tail && r <= newest;
                 bool absent = false;                                // a page that is none: its rows do not count
 #pragma unroll
                 for (int x = 0; x < U; ++x) absent = absent || !present(pv[x]);
                 absent = __any(absent);
-                if (!MORE && fresh) {                               // the newest row's key takes its place among the rows
+                if (with_new) {                                     // the newest row's key takes its place among the rows
 #pragma unroll
                     for (int x = 0; x < U; ++x)
 #pragma unroll
@@ -357,6 +393,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                             for (int k = 0; k < NK; ++k) kr[x][t][k] = *reinterpret_cast<const uint4*>(&sh.new_k[k * 4 * QE + g * QE]);
                         }
                 }
+                const uint4* q_at = q_lds;
+                int none = 0;                                       // (read again in every turn: the compiler cannot know that it is 0)
+                asm volatile("" : "+v"(none));
+                q_at += none;
+                uint4 qr[(P::ES == 2 ? 2 : 1) * NK];
+#pragma unroll
+                for (int k = 0; k < (P::ES == 2 ? 2 : 1) * NK; ++k) qr[k] = q_at[k * 64];
                 float s[U][R];
 #pragma unroll
                 for (int x = 0; x < U; ++x)
@@ -367,14 +410,14 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         for (int k = 0; k < NK; ++k) {
                             if constexpr (P::ES == 2) {
                                 const half8 kv = __builtin_bit_cast(half8, kr[x][t][k]);
-                                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, qh[k], d, 0, 0, 0);
-                                d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, ql[k], d1, 0, 0, 0);
+                                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, __builtin_bit_cast(half8, qr[2 * k]), d, 0, 0, 0);
+                                d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, __builtin_bit_cast(half8, qr[2 * k + 1]), d1, 0, 0, 0);
                             } else {
                                 const f32x4 kv = __builtin_bit_cast(f32x4, kr[x][t][k]);
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
-                                    if (e & 1) d1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[e], qf[k][e], d1, 0, 0, 0);
-                                    else d = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[e], qf[k][e], d, 0, 0, 0);
+                                    if (e & 1) d1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[e], __builtin_bit_cast(f32x4, qr[k])[e], d1, 0, 0, 0);
+                                    else d = __builtin_amdgcn_mfma_f32_16x16x4f32(kv[e], __builtin_bit_cast(f32x4, qr[k])[e], d, 0, 0, 0);
                                 }
                             }
                         }
@@ -384,11 +427,11 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                 __builtin_amdgcn_sched_barrier(0);
                 int pk2[U], pv2[U];
                 if constexpr (MORE) {
-                    load_pages(r + 2 * P::CH, pk2, pv2);
-                    issue_k(r + P::CH, pk1);
+                    load_pages(after(next_r), pk2, pv2);
+                    issue_k(next_r, pk1);
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if ((!MORE && tail) || absent) {
+                if (tail || absent) {
 #pragma unroll
                     for (int x = 0; x < U; ++x)
 #pragma unroll
@@ -417,21 +460,23 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         s[x][e] = __builtin_amdgcn_exp2f(s[x][e] - sub);
                         l += s[x][e];
                     }
-                if ((!MORE && tail) || absent) {                    // rows that do not count hold anything: 0 times it must be 0
+                if (tail || absent) {                               // rows that do not count hold anything: 0 times it must be 0
 #pragma unroll
                     for (int x = 0; x < U; ++x) {
                         const int row0 = r + x * RG + R * g;
+                        const bool in_unit = with_new && newest >= row0 && newest < row0 + R;
 #pragma unroll
                         for (int d = 0; d < ND; ++d) {
                             T v[R];
                             __builtin_memcpy(v, &vr[x][d], 16);
                             T own{};
-                            if (!MORE && fresh) own = sh.new_v[d * 16 + i];
+                            if (with_new) own = sh.new_v[d * 16 + i];
 #pragma unroll
-                            for (int e = 0; e < R; ++e) {
-                                if (!MORE && fresh && row0 + e == newest) v[e] = own;
+                            for (int e = 0; e < R; ++e)
+                                if (in_unit && row0 + e == newest) v[e] = own;
+#pragma unroll
+                            for (int e = 0; e < R; ++e)
                                 if (!present(pv[x]) || row0 + e >= len) v[e] = (T)0.f;
-                            }
                             __builtin_memcpy(&vr[x][d], v, 16);
                         }
                     }
@@ -440,11 +485,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                 for (int x = 0; x < U; ++x) {
                     if constexpr (P::ES == 2) {
                         half8 ph, pl;
-#pragma unroll
-                        for (int e = 0; e < R; ++e) {
-                            ph[e] = (_Float16)s[x][e];
-                            pl[e] = (_Float16)(s[x][e] - (float)ph[e]);
-                        }
+                        split_half8(s[x], ph, pl);
 #pragma unroll
                         for (int d = 0; d < ND; ++d) acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, vr[x][d]), ph, acc[d], 0, 0, 0);
 #pragma unroll
@@ -458,12 +499,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if constexpr (MORE) {
-                    issue_v(r + P::CH, pv1);
+                    issue_v(next_r, pv1);
+                    r = next_r;
 #pragma unroll
                     for (int x = 0; x < U; ++x) { pv[x] = pv1[x]; pk1[x] = pk2[x]; pv1[x] = pv2[x]; }
                 }
             };
-            for (; r + P::CH < rend; r += P::CH) turn(std::true_type());
+            for (int more = turns; more > 1; --more) turn(std::true_type());
             turn(std::false_type());
             l = reduce_halves(reduce_row_pairs(l, AddOp()), AddOp());
         }
