@@ -390,7 +390,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         for (int t = 0; t < KT; ++t) {
                             if (r + x * RG + R * (i >> 2) + 4 * t + (i & 3) != newest) continue;
 #pragma unroll
-                            for (int k = 0; k < NK; ++k) kr[x][t][k] = *reinterpret_cast<const uint4*>(&sh.new_k[k * 4 * QE + g * QE]);
+                            for (int k = 0; k < NK; ++k) __builtin_memcpy(&kr[x][t][k], &sh.new_k[k * 4 * QE + g * QE], 16);
                         }
                 }
                 const uint4* q_at = q_lds;
@@ -511,6 +511,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
         }
 
         // ---- merge the waves ----
+        asm volatile("" ::: "memory");                              // outputs take the place of q
         if (i < nh) {
             if (g == 0) { sh.m[i][wave] = m; sh.l[i][wave] = l; }
 #pragma unroll

@@ -181,20 +181,28 @@ template <int E, typename S> __device__ __forceinline__ void load_many(const S* 
     constexpr int N = 16 / sizeof(S);
 #pragma unroll
     for (int e = 0; e < E; e += N) {
-        alignas(16) S t[N];
-        *reinterpret_cast<u32x4*>(t) = *reinterpret_cast<const u32x4*>(p + e);
+        S t[N];
+        const uint4 v = *reinterpret_cast<const uint4*>(p + e);
+        __builtin_memcpy(t, &v, 16);
 #pragma unroll
         for (int j = 0; j < N; ++j) { if constexpr (std::is_same<S, bf16_t>::value) y[e + j] = bf16_to_f32(t[j]); else y[e + j] = (float)t[j]; }
     }
 }
 template <int E, typename T> __device__ __forceinline__ void store_many(T* p, const float (&y)[E]) {
-    alignas(16) T t[E];
+    T t[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) t[e] = held<T>(y[e]);
-    if constexpr (E * sizeof(T) == 8) *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(t);
-    else {
+    if constexpr (E * sizeof(T) == 8) {
+        uint2 v;
+        __builtin_memcpy(&v, t, 8);
+        *reinterpret_cast<uint2*>(p) = v;
+    } else {
 #pragma unroll
-        for (int e = 0; e < E; e += 16 / sizeof(T)) *reinterpret_cast<uint4*>(p + e) = *reinterpret_cast<const uint4*>(t + e);
+        for (int e = 0; e < E; e += 16 / sizeof(T)) {
+            uint4 v;
+            __builtin_memcpy(&v, t + e, 16);
+            *reinterpret_cast<uint4*>(p + e) = v;
+        }
     }
 }
 // N = 1 or 2 adjacent elements
@@ -280,10 +288,12 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
         T* to = pool_at(a.v_pages, at) + ((at & row_mask) / R * HD + lane * DL) * R;
 #pragma unroll
         for (int d = 0; d < DL; ++d) {
-            alignas(16) T unit[R];
+            T unit[R];
 #pragma unroll
             for (int e = 0; e < R; ++e) unit[e] = held<T>(y[e][d]);
-            *reinterpret_cast<uint4*>(to + d * R) = *reinterpret_cast<const uint4*>(unit);
+            uint4 v;
+            __builtin_memcpy(&v, unit, 16);
+            *reinterpret_cast<uint4*>(to + d * R) = v;
         }
     }
     for (unsigned left = valid & ~covered & own; left; left &= left - 1) {

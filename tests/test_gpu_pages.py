@@ -164,6 +164,67 @@ def test_attention_against_64_bits(case):
     assert torch.equal(out, cache.attend(0, q, k if new else None, v if new else None, rope_cs=cs))       # the same bits again
 
 
+@pytest.mark.parametrize("heads,group,hd,kv,act,page_rows", [(8, 1, 128, "f16", "f32", 32), (8, 4, 128, "f32", "f32", 16), (16, 2, 64, "f16", "bf16", 64), (8, 3, 64, "f32", "f16", 16)])
+@pytest.mark.parametrize("order", ["random", "in order"])
+def test_attention_runs_of_many_chunks(heads, group, hd, kv, act, page_rows, order):
+    """More rows than a chunk for every workgroup: runs of many turns that begin anywhere in their circle, end inside sequences and hold several, with pages a power of two apart too."""
+    import torch
+    rng = np.random.RandomState(hd + heads)
+    lens = [2048] * 12 + [2049, 2047, 0, 1] + rng.randint(1500, 2600, 20).tolist() + rng.randint(1, 200, 12).tolist()
+    cache, g = _cache(lens, heads, group, hd, kv, page_rows, seed=21, fill="nan", spare=0)
+    if order == "in order":
+        flat = torch.full_like(cache.tables, -1)
+        at = 0
+        for b, n in enumerate(lens):
+            m = -(-n // page_rows)
+            flat[b, :m] = torch.arange(at, at + m)
+            at += m
+        rows_k, rows_v = ([_as_rows(cache, p)[0, _slots(cache, b, range(n))] for b, n in enumerate(lens)] for p in (cache.k_pages, cache.v_pages))
+        cache.tables.copy_(flat)
+        for pool, rows in ((cache.k_pages, rows_k), (cache.v_pages, rows_v)):
+            whole = torch.full_like(_as_rows(cache, pool), math.nan)
+            for b, n in enumerate(lens):
+                whole[0, _slots(cache, b, range(n))] = rows[b]
+            _from_rows(cache, pool, whole)
+    t = _types()[act]
+    q = torch.empty(len(lens), heads * group, hd, dtype=t, device=DEV).normal_(generator=g)
+    k, v = (torch.empty(len(lens), heads, hd, dtype=t, device=DEV).normal_(generator=g) for _ in range(2))
+    before = [_as_rows(cache, p)[0] for p in (cache.k_pages, cache.v_pages)]
+    out = cache.attend(0, q, k, v)
+    live = [b for b, n in enumerate(lens) if n]
+    at = torch.cat([_slots(cache, b, [lens[b] - 1]) for b in live])
+    for was, pool, x in zip(before, (cache.k_pages, cache.v_pages), (k, v)):
+        was[at] = x[live].clamp(-HALF_MAX, HALF_MAX).to(pool.dtype)
+        now = _as_rows(cache, pool)[0]
+        assert torch.equal(now.view(torch.uint8), was.view(torch.uint8))
+    _check(out, *_reference(cache, q.double(), lens))
+
+
+def test_attention_of_thousands_of_sequences():
+    import torch
+    lens = [(b * 7919) % 23 if b % 3 else 0 for b in range(4096)]
+    from paper_2503_08524_amd import PagedCache
+    g = torch.Generator(device=DEV)
+    g.manual_seed(22)
+    cache = PagedCache(2, 1, 64, 8192, 16, 4096, 2, device=DEV)
+    slots = cache.reserve(torch.tensor(lens, dtype=torch.int32, device=DEV), sum(lens))[1]
+    assert cache.rows.tolist() == lens
+    k, v = (torch.empty(sum(lens), 1, 64, device=DEV).normal_(generator=g) for _ in range(2))
+    cache.append(0, slots, k, v)
+    q = torch.empty(4096, 2, 64, device=DEV).normal_(generator=g)
+    out = cache.attend(0, q)
+    # the same in 64 bits with every sequence padded to 22 rows
+    n = torch.tensor(lens, device=DEV)
+    first = torch.cat([torch.zeros(1, dtype=torch.long, device=DEV), n.cumsum(0)])[:-1]
+    p = torch.arange(22, device=DEV)
+    at = (first[:, None] + p).clamp(max=sum(lens) - 1)
+    kk, vv = k.half().double()[at][:, :, 0], v.half().double()[at][:, :, 0]
+    s = (torch.matmul(q.double(), kk.transpose(1, 2)) / 8).masked_fill((p >= n[:, None])[:, None], -math.inf)
+    want = torch.nan_to_num(torch.matmul(torch.softmax(s, -1), vv))
+    assert (out.double() - want).abs().max() <= 2e-4 * v.abs().max()         # sum |q k| / 8 below 20: see _reference
+    assert not out[n == 0].any()
+
+
 def test_attention_scale_layers_strides_and_an_output_with_gaps():
     import torch
     heads, group, hd, lens = 2, 2, 128, [40, 300, 0, 9]
