@@ -223,10 +223,6 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
         if (c1 <= 0) return;                                        // the run ends in what this one counts more
         const int kvh = tiles == 1 ? hh : small_quotient(hh, tiles), h0 = (hh - kvh * tiles) * kPagedHeads, nh = min(kPagedHeads, a.group - h0);
         const bool whole = c0 == 0 && c1 == chunks;
-        // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
-        const int w0 = whole ? run : runs.of(head_begin + over), parts = whole ? 1 : runs.of(head_begin + per_head - 1) - w0 + 1;
-        const unsigned before = runs.begin(w0) < head_begin ? 1 : 0;
-        auto slot_of = [&](int k) { return 2u * (w0 + k) + (k == 0 ? before : 0); };
         const int newest = len - 1, last_block = newest / R;
         const int* tab = a.tables + (size_t)b * a.table_stride;
         char* Kh = static_cast<char*>(a.k_pages) + kvh * head_bytes;
@@ -460,24 +456,38 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         s[x][e] = __builtin_amdgcn_exp2f(s[x][e] - sub);
                         l += s[x][e];
                     }
-                if (tail || absent) {                               // rows that do not count hold anything: 0 times it must be 0
+                if (tail || absent) {
+                    // Rows that do not count hold anything: 0 times it must be 0.  Bits of a lane's R rows in the four words of a unit, the same in all its units.
+                    constexpr int PER = 4 / P::ES;                  // rows of a word
+                    constexpr uint32_t ROW = PER == 2 ? 0xffffu : 0xffffffffu;
 #pragma unroll
                     for (int x = 0; x < U; ++x) {
                         const int row0 = r + x * RG + R * g;
-                        const bool in_unit = with_new && newest >= row0 && newest < row0 + R;
+                        uint32_t counts[4], fresh_bits[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            counts[j] = fresh_bits[j] = 0;
+#pragma unroll
+                            for (int e = 0; e < PER; ++e) {
+                                counts[j] |= present(pv[x]) && row0 + j * PER + e < len ? ROW << (16 * e) : 0u;
+                                fresh_bits[j] |= row0 + j * PER + e == newest ? ROW << (16 * e) : 0u;
+                            }
+                        }
+                        if (with_new) {                             // the newest row's value takes its place
+#pragma unroll
+                            for (int d = 0; d < ND; ++d) {
+                                uint32_t own = 0;
+                                __builtin_memcpy(&own, &sh.new_v[d * 16 + i], P::ES);
+                                if (PER == 2) own |= own << 16;
+                                vr[x][d].x = (fresh_bits[0] & own) | (~fresh_bits[0] & vr[x][d].x);
+                                vr[x][d].y = (fresh_bits[1] & own) | (~fresh_bits[1] & vr[x][d].y);
+                                vr[x][d].z = (fresh_bits[2] & own) | (~fresh_bits[2] & vr[x][d].z);
+                                vr[x][d].w = (fresh_bits[3] & own) | (~fresh_bits[3] & vr[x][d].w);
+                            }
+                        }
 #pragma unroll
                         for (int d = 0; d < ND; ++d) {
-                            T v[R];
-                            __builtin_memcpy(v, &vr[x][d], 16);
-                            T own{};
-                            if (with_new) own = sh.new_v[d * 16 + i];
-#pragma unroll
-                            for (int e = 0; e < R; ++e)
-                                if (in_unit && row0 + e == newest) v[e] = own;
-#pragma unroll
-                            for (int e = 0; e < R; ++e)
-                                if (!present(pv[x]) || row0 + e >= len) v[e] = (T)0.f;
-                            __builtin_memcpy(&vr[x][d], v, 16);
+                            vr[x][d].x &= counts[0]; vr[x][d].y &= counts[1]; vr[x][d].z &= counts[2]; vr[x][d].w &= counts[3];
                         }
                     }
                 }
@@ -512,17 +522,26 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 
         // ---- merge the waves ----
         asm volatile("" ::: "memory");                              // outputs take the place of q
-        if (i < nh) {
+        // From here on addresses are computed where they are used (the compiler cannot know that `none` and `still` are 0 and tid): ahead of the loop over (sequence, heads), where it
+        // would compute them, every launch waits for them before its first load, and they spill.
+        int none = 0, still = tid;
+        asm volatile("" : "+s"(none));
+        asm volatile("" : "+v"(still));
+        const int H_ = H + none, HH_ = HH + none, GP_ = GP + none;
+        if (const int i = still & 15, g = (still & 63) >> 4; i < nh) {
             if (g == 0) { sh.m[i][wave] = m; sh.l[i][wave] = l; }
 #pragma unroll
             for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(&sh.o[wave][i][d * 16 + g * 4]) = acc[d];
         }
         __syncthreads();
-        // From here on addresses are computed where they are used (the compiler cannot know that `none` is 0): ahead of the loop over (sequence, heads), where it would compute
-        // them, every launch waits for them before its first load, and they spill.
-        int none = 0;
-        asm volatile("" : "+s"(none));
-        const int H_ = H + none, HH_ = HH + none, GP_ = GP + none;
+        // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
+        int w0 = run, parts = 1;
+        if (!whole) {
+            w0 = runs.of(head_begin + over);
+            parts = runs.of(head_begin + per_head - 1) - w0 + 1;
+        }
+        const unsigned before = runs.begin(w0) < head_begin ? 1 : 0;
+        auto slot_of = [&](int k) { return 2u * (w0 + k) + (k == 0 ? before : 0); };
         const int items = nh * (HD / 4);                            // a thread has four dims of a head
         auto finish = [&](int h, int t, const float (&o)[4], float sum) {
             const float by = sum == 0.f ? 0.f : 1.f / sum;          // no row counted: zeros
@@ -539,7 +558,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             st_agent2(part_o_at(slot, h, t + 2), o[2], o[3]);
             if (t == 0) st_agent2(part_ml_at(slot, h), M, L);
         };
-        for (int idx = tid; idx < items; idx += 256) {
+        for (int idx = still; idx < items; idx += 256) {
             const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
             const f32x4 ms = *reinterpret_cast<const f32x4*>(sh.m[h]), ls = *reinterpret_cast<const f32x4*>(sh.l[h]);
             f32x4 x[4];
@@ -562,7 +581,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             auto arrive = [&](int* ticket, int of) {
                 wait_stores();
                 __syncthreads();
-                if (tid == 0) {
+                if (still == 0) {
                     sh.is_last = atomicAdd(ticket, 1) == of - 1;
                     if (sh.is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // all arrived: leave it clean
                 }
@@ -573,7 +592,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                 constexpr int J = decltype(flight)::value;          // partial results in flight
 #pragma unroll
                 for (int it = 0; it < ITEMS; ++it) {
-                    const int idx = tid + it * 256, h = idx / (HD / 4), t = idx % (HD / 4) * 4;
+                    const int idx = still + it * 256, h = idx / (HD / 4), t = idx % (HD / 4) * 4;
                     if (idx >= items) break;
                     float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
                     for (int k0 = 0; k0 < count; k0 += J) {
@@ -620,7 +639,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                     __syncthreads();
 #pragma unroll
                     for (int it = 0; it < ITEMS; ++it) {
-                        const int idx = tid + it * 256;
+                        const int idx = still + it * 256;
                         if (idx >= items) break;
                         const float o[4] = {js[it][0], js[it][1], js[it][2], js[it][3]};
                         publish(slot_of(first), idx / (HD / 4), idx % (HD / 4) * 4, o, js[it][4], js[it][5]);
