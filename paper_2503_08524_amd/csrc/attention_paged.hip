@@ -271,20 +271,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 #pragma unroll
         for (int d = 0; d < ND; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (turns > 0) {
-            A nk[2], nv[2];                                         // dims `lane` and lane + HD / 2 of the newest row
-            float2 ncs = {1.f, 0.f};
-            if (fresh) {
-                const long long at = b * a.kv_stride + (long long)kvh * HD + lane % (HD / 2);
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    nk[e] = static_cast<const A*>(a.k_new)[at + e * (HD / 2)];
-                    nv[e] = static_cast<const A*>(a.v_new)[at + e * (HD / 2)];
-                }
-                if (a.rope_cs) ncs = a.rope_cs[(size_t)b * (HD / 2) + lane % (HD / 2)];
-            }
-            int pk[U], pv[U], pk1[U], pv1[U];
+            int pk[U], pv[U], pk1[U], pv1[U], new_page = 0;
             load_pages(r, pk, pv);
-            load_pages(after(r), pk1, pv1);
+            if (fresh) new_page = tab[last_block >> block_shift];
             float qf[NK][QE];
             ActVec<QE, A> qa[NK];
 #pragma unroll
@@ -295,10 +284,20 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 #pragma unroll
                 for (int k = 0; k < NK / 2; ++k) cs[k].load(reinterpret_cast<const float*>(a.rope_cs + (size_t)b * (HD / 2) + k * 4 * QE + g * QE));
             }
-            const int new_page = tab[last_block >> block_shift];
-            uint4 unit[2];                                          // the values of dims `lane` and lane + HD / 2 beside the newest row's: R rows share 16 bytes
-            char* const unit_at = Vh + (size_t)(present(new_page) ? new_page : 0) * page_bytes + ((last_block & block_mask) * HD + lane % (HD / 2)) * 16;
+            load_pages(after(r), pk1, pv1);
+            A nk[2], nv[2];                                         // dims `lane` and lane + HD / 2 of the newest row
+            float2 ncs = {1.f, 0.f};
+            uint4 unit[2];                                          // and the values beside it: R rows share 16 bytes
+            char* unit_at = Vh;
             if (fresh) {
+                const long long at = b * a.kv_stride + (long long)kvh * HD + lane % (HD / 2);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    nk[e] = static_cast<const A*>(a.k_new)[at + e * (HD / 2)];
+                    nv[e] = static_cast<const A*>(a.v_new)[at + e * (HD / 2)];
+                }
+                if (a.rope_cs) ncs = a.rope_cs[(size_t)b * (HD / 2) + lane % (HD / 2)];
+                unit_at += (size_t)(present(new_page) ? new_page : 0) * page_bytes + ((last_block & block_mask) * HD + lane % (HD / 2)) * 16;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) unit[e] = *reinterpret_cast<const uint4*>(unit_at + e * (HD * 8));
             }
