@@ -239,7 +239,8 @@ int d3_truncate(d3_ctx *ctx, int32_t n_rows);
  * [0, n_pages) in a table is a page that is not there: its rows count as masked.  A slot outside the pool is skipped.
  * A row may be given to one slot at a time (two rows of one call with the same slot: either is kept, element by element).
  * Calls on one d3_pages must be ordered (one stream, or streams that wait for each other; replays of graphs too): they share
- * its workspace, and they read what the ones before wrote. */
+ * its workspace, and they read what the ones before wrote.  Two handles on the same pools, each with a workspace of its own, may
+ * be used at the same time as far as neither writes what the other reads. */
 typedef struct {
     int32_t n_layers, n_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128; n_heads % n_kv_heads == 0 */
     int32_t kv_dtype;                                  /* D3_F16 or D3_F32, see d3_model_desc */
@@ -281,7 +282,7 @@ int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n,
  * q, out: dev [B][n_heads][head_dim] of `dtype`, sequence b at b * q_stride, b * out_stride.  k_new, v_new: dev [B][H_kv][head_dim] of `dtype` at b * kv_stride, or both NULL.
  * Given, they are row rows[b] - 1, which the call also writes to its page (which no other sequence of the call may list); else that row is there already.  rope_cs: dev float [B][head_dim / 2][2]: q and
  * k_new turn by it; NULL: neither does.  q, k_new, v_new, rope_cs 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
- * Keys and values are used as the pool holds them; sums and softmax in 32 bits. */
+ * out may be q itself.  Keys and values are used as the pool holds them; sums and softmax in 32 bits. */
 int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,
                        int64_t kv_stride, const float *rope_cs, const int32_t *tables, const int32_t *rows, float scale, void *out,
                        int64_t out_stride, void *hip_stream);

@@ -20,8 +20,6 @@ template <typename T> __device__ __forceinline__ T held(float v);
 template <> __device__ __forceinline__ float held<float>(float v) { return v; }
 template <> __device__ __forceinline__ f16_t held<f16_t>(float v) { return (f16_t)(v != v ? v : fminf(fmaxf(v, -65504.f), 65504.f)); }
 
-inline int unit_rows(int kv_dtype) { return 16 / kv_elem_bytes(kv_dtype); }
-
 struct ReserveArgs {
     int B, max_pages, n_pages, page_shift, max_tokens;
     const int32_t *added, *rows_in, *n_free_in;

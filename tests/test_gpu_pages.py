@@ -597,6 +597,35 @@ def test_calls_on_another_stream():
     assert torch.equal(got, want)
 
 
+def test_two_handles_on_the_same_pools_at_the_same_time():
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    lens = [700, 90, 0, 4000]
+    cache, g = _cache(lens, 2, 4, 128, "f16", 16, seed=12)
+    shared = dict(k_pages=cache.k_pages, v_pages=cache.v_pages, tables=cache.tables, rows=cache.rows, free_pages=cache.free_pages, n_free=cache.n_free)
+    other = PagedCache(8, 2, 128, cache.n_pages, 16, 4, cache.max_pages, device="cuda", **shared)
+    q = torch.empty(4, 8, 128, device=DEV).normal_(generator=g)
+    want = cache.attend(0, q)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    outs = [[torch.empty_like(q) for _ in range(30)] for _ in streams]
+    for k in range(30):
+        for c, s, o in zip((cache, other), streams, outs):
+            with torch.cuda.stream(s):
+                c.attend(0, q, out=o[k])
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for o in outs for x in o)
+
+
+def test_attention_writes_over_its_queries():
+    import torch
+    for act, lens in (("f32", [700, 90, 0, 4000]), ("bf16", [2000] * 40)):
+        cache, g = _cache(lens, 2, 20, 64, "f16", 16, seed=13)
+        q = torch.empty(len(lens), 40, 64, dtype=_types()[act], device=DEV).normal_(generator=g)
+        want = cache.attend(0, q)
+        assert cache.attend(0, q, out=q) is q and torch.equal(q, want)
+
+
 def test_refusals():
     import torch
     from paper_2503_08524_amd import D3Error, PagedCache
@@ -605,7 +634,7 @@ def test_refusals():
     q, k = torch.zeros(3, 4, 64, device=DEV), torch.zeros(3, 2, 64, device=DEV)
     slots = ints(0, 1, 2)
     for call in (lambda: cache.reserve(ints(1, 1, 1, 1), 4), lambda: cache.reserve(torch.ones(3, device=DEV), 4), lambda: cache.reserve(ints(1), 4, slots=ints(0)),
-                 lambda: cache.reserve(ints(1), -1), lambda: cache.reserve(torch.ones(1, dtype=torch.int32), 1),
+                 lambda: cache.reserve(ints(1), -1), lambda: cache.reserve(ints(1, 1, 1, 1)[::2], 4), lambda: cache.reserve(torch.ones(1, dtype=torch.int32), 1),
                  lambda: cache.append(0, slots, k, k[:2]), lambda: cache.append(0, slots, k, k.half()), lambda: cache.append(0, slots.long(), k, k),
                  lambda: cache.append(0, slots, k.double(), k.double()), lambda: cache.append(0, slots, k, k, rope_cs=torch.zeros(3, 64, device=DEV)),
                  lambda: cache.attend(0, k), lambda: cache.attend(0, q, k), lambda: cache.attend(0, q, k.half(), k.half()), lambda: cache.attend(0, q, out=q.half()),
