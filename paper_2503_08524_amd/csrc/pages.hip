@@ -9,7 +9,7 @@ namespace {
 
 // ---------------- page tables and slot maps ----------------
 // One workgroup: sums over the sequences (a wave's by row shifts, no LDS; the waves' through LDS), then pages and tokens found in those sums by bisection.  A chain of round trips
-// bounds it: requests in, sums, pages of the stack, tables, slots.
+// bounds it: requests in, sums, pages of the stack, tables, slots (8 sequences 2.4 us, 256 with 20000 new rows 6.2 and 3.7 for the slots).
 __device__ __forceinline__ unsigned long long shifted64(unsigned long long v, int which) {
     unsigned lo, hi;
 #define D3_SHIFT(ctrl, rows) lo = __builtin_amdgcn_update_dpp(0, (unsigned)v, ctrl, rows, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (unsigned)(v >> 32), ctrl, rows, 0xf, false)
@@ -223,6 +223,8 @@ template <int N, typename S> __device__ __forceinline__ void load_few(const S* p
 // Of a value's dims R rows lie side by side in 16 bytes.  A lane has one or two dims: where a token is row 0 of a unit of R rows that follow each other in
 // `slots`, its wave loads those R rows (whole lines each) and writes the unit's 16 bytes per dim, for all of them, also those of the next wave's tokens;
 // only rows of units that the call does not fill are written element by element.  What each token is, is one wave's business: bits of a mask.
+// Bound by memory: 8 layers x 1024 rows of 8 heads of 128, fp32, 30.5 us = 4.4 TB/s moved (a large copy 4.7); 512 rows of 32 heads, fp32 to fp16 with rotation, 6.7 us.  Through LDS,
+// 64 tokens a workgroup, the values took 52 and 28 us.
 constexpr int kAppendTokens = 32;
 
 template <typename S, typename T, int HD>
@@ -308,7 +310,8 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
 
 // ---------------- missing-state fill on pages ----------------
 // A wave has one (token, KV head): 16 bytes of the key in the first lanes, one or two elements of the value in each, read once from the source block
-// and written into a few of the dropped ones (grid.y).
+// and written into a few of the dropped ones (grid.y).  40 blocks of 8 rows of 8 heads, fp32, 4.7 us: little more than a launch, though the values, four bytes in every 16, write 6.5 MB
+// for 2.6.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void pages_fill_kernel(PagesFillArgs a, int layers_each) {
     constexpr int R = 16 / sizeof(T), DL = HD / 64;

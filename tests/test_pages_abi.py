@@ -68,3 +68,19 @@ def test_null_handles_are_errors(lib):
                    lib.d3_decode_step_paged(None, None, None, 1, 1, None, None, None, None, None, None), lib.d3_fill_missing_paged(None, None, 1, 1, None, None)):
         assert status == -1
     assert lib.d3_pages_destroy(None) == 0
+
+
+def test_attention_keeps_its_rows_in_registers(tmp_path):
+    """Two workgroups of four waves a compute unit have 256 registers a lane; with spills in the loop over rows the attention takes twice as long, and nothing else shows it."""
+    import os
+    import re
+    import subprocess
+    out = str(tmp_path / "attention_paged.s")
+    flags = [f for f in d3_build.FLAGS if f != "-fPIC"]
+    subprocess.run([d3_build.HIPCC] + flags + ["-x", "hip", "-S", "--offload-device-only", os.path.join(d3_build.CSRC, "attention_paged.hip"), "-o", out], check=True, capture_output=True)
+    text = open(out).read()
+    kernels = re.findall(r"\.name:\s+(\S*attn_paged_kernel\S*)", text)
+    assert len(set(kernels)) == 8
+    for field, most in ((".private_segment_fixed_size", 0), (".vgpr_spill_count", 0), (".vgpr_count", 256)):
+        found = [int(x) for x in re.findall(re.escape(field) + r":\s+(\d+)", text)]
+        assert len(found) == 8 and max(found) <= most, (field, found)
