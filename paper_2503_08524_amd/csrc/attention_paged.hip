@@ -3,7 +3,7 @@
 // each sequence with a length and a list of pages of its own.
 //
 // Work: the rows of every (sequence, KV head, 16 query heads) are cut into chunks of 64 KB of keys and values, all chunks laid end to end, and
-// every workgroup takes an equal run of them, whatever the lengths: it may end one sequence, take others whole and begin another.  The host
+// every workgroup (or wave, see attn_paged_kernel) takes an equal run of them, whatever the lengths: it may end one sequence, take others whole and begin another.  The host
 // knows no lengths, so a launch can be captured once and replayed while sequences grow.  A run that covers a (sequence, heads) whole writes the
 // result; else it publishes (max, sum, unnormalised output), and the run that arrives last joins them.
 //
@@ -50,7 +50,7 @@ template <typename T, int HD>
 struct __align__(16) PagedShared {
     float o[4][kPagedHeads][HD + 4];               // per wave: unnormalised outputs (rows 4 words apart in the banks)
     float m[kPagedHeads][4], l[kPagedHeads][4];    // per wave: running max and sum of each head
-    T new_k[HD], new_v[HD];                        // the newest row as the pool holds it
+    T new_k[4][HD], new_v[4][HD];                  // per wave: the newest row as the pool holds it
     int is_last;
 };
 
@@ -160,34 +160,53 @@ __device__ __forceinline__ void paged_take_args(const PagedAttnArgs& a) {
     asm volatile("" :: "s"(a.dtype), "s"(a.scale), "s"(a.out), "s"(a.out_stride), "s"(a.out_split), "s"(a.out_form.lo), "s"(a.part_o), "s"(a.part_ml), "s"(a.tickets), "s"(a.by_runs.d), "s"(a.by_runs.m));
 }
 
-// T: the pool's type; A: float, or the bits of a 16-bit type (q, k_new, v_new)
-template <typename T, int HD, typename A>
-__global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
+// What is known of the lengths before the work is divided.
+struct Lengths {
+    int chunks, turns, live;                                        // chunks (four waves' turns) and turns (one's) of all sequences; sequences that have rows
+    float shortest;                                                 // rows of the shortest of these (to 24 bits)
+    int own;                                                        // the length of sequence `lane`
+};
+template <typename P, typename Length>
+__device__ __forceinline__ Lengths take_lengths(int B, int lane, Length length) {
+    Lengths n = {0, 0, 0, 0x1p30f, lane < B ? length(lane) : 0};
+    auto take = [&](int len) {
+        n.chunks += (len + P::CH - 1) / P::CH;
+        n.turns += (len + P::TR - 1) / P::TR;
+        n.live += __popcll(__ballot(len > 0));
+        n.shortest = fminf(n.shortest, len > 0 ? (float)len : 0x1p30f);
+    };
+    take(n.own);
+    for (int b0 = 64; b0 < B; b0 += 512) {                          // eight of a lane's in flight (3000 sequences of one KV head 65 -> 52 us)
+        int len[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) len[j] = length(min(b0 + j * 64 + lane, B - 1));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) take(b0 + j * 64 + lane < B ? len[j] : 0);
+    }
+    n.chunks = __builtin_amdgcn_readlane(scan_wave(n.chunks), 63);
+    n.turns = __builtin_amdgcn_readlane(scan_wave(n.turns), 63);
+    n.shortest = -reduce_row(reduce_row_pairs(reduce_halves(-n.shortest, MaxOp()), MaxOp()), MaxOp());
+    n.shortest = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(n.shortest)));
+    return n;
+}
+
+// T: the pool's type; A: float, or the bits of a 16-bit type (q, k_new, v_new).  WAVES: a chunk is one wave's turn and a run a wave's; else a chunk is a turn of each of the four waves of a
+// workgroup, whose run it is.
+template <typename T, int HD, typename A, bool WAVES, typename Length>
+__device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedShared<T, HD>& sh, const Lengths& lengths, Length length) {
     typedef PagedShape<T, HD> P;
-    constexpr int R = P::R, KT = P::KT, RG = P::RG, NK = P::NK, ND = P::ND, U = P::U, QE = P::QE;
-    __shared__ PagedShared<T, HD> sh;
-    paged_take_args(a);
+    constexpr int R = P::R, KT = P::KT, RG = P::RG, NK = P::NK, ND = P::ND, U = P::U, QE = P::QE, CH = WAVES ? P::TR : P::CH;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
     const int H = a.H_kv * a.group, tiles = (a.group + kPagedHeads - 1) / kPagedHeads, HH = a.H_kv * tiles, GP = min(a.group, kPagedHeads);
-    auto length = [&](int b) { return min(max(a.rows[b], 0), a.max_rows); };
+    const Divisor& by_runs = WAVES ? a.by_waves : a.by_runs;
 
-    // ---- this workgroup's run of units, and where it begins ----
-    // Lane x has sequence b0 + x.  A (sequence, heads) counts as its chunks, and where runs are longer than the shortest one, i.e. may hold several, as `over` more: what beginning
+    // ---- this run of units, and where it begins ----
+    // A (sequence, heads) counts as its chunks, and where runs are longer than the shortest one, i.e. may hold several, as `over` more: what beginning
     // and ending it costs (48 requests of 1 to 32768 rows 130 -> 110 us).  Elsewhere that would only make runs uneven (20480 rows, 32 heads: 160 chunks are 10 a workgroup; 57.8 us, with `over` 62.3).
-    int len_of = lane < a.B ? length(lane) : 0;
-    int total = 0, live = 0;
-    float shortest = INFINITY;                                      // of up to 2^24 chunks
-    bool idle = false;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int len = b0 == 0 ? len_of : b0 + lane < a.B ? length(b0 + lane) : 0, c = (len + P::CH - 1) / P::CH;
-        total += __builtin_amdgcn_readlane(scan_wave(c), 63);
-        live += __popcll(__ballot(len > 0));
-        idle = idle || __any(b0 + lane < a.B && len == 0);
-        shortest = fminf(shortest, -reduce_row(reduce_row_pairs(reduce_halves(len > 0 ? -(float)c : -INFINITY, MaxOp()), MaxOp()), MaxOp()));
-    }
-    const int over = (float)(total * HH) > (float)gridDim.x * __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(shortest))) ? kPagedOverhead : 0;
-    total = (total + live * over) * HH;
-    if (idle) {
+    auto chunks_of = [&](int len) { return (len + CH - 1) / CH; };
+    const int chunks_in_all = WAVES ? lengths.turns : lengths.chunks;
+    const int over = (float)(chunks_in_all * HH) > (float)by_runs.d * (float)chunks_of((int)lengths.shortest) ? kPagedOverhead : 0, total = (chunks_in_all + lengths.live * over) * HH;
+    if (lengths.live < a.B) {
         for (int b = blockIdx.x; b < a.B; b += gridDim.x) {         // a sequence without rows: zeros
             if (length(b) > 0) continue;
             const float zero[4] = {0.f, 0.f, 0.f, 0.f};
@@ -197,23 +216,44 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             }
         }
     }
-    const Runs runs(total, a.by_runs);
-    const int run = blockIdx.x, end = runs.begin(run + 1);
+    if (total == 0) return;
+    const Runs runs(total, by_runs);
+    const int run = WAVES ? blockIdx.x * 4 + wave : blockIdx.x, end = runs.begin(run + 1);
     int u = runs.begin(run);
     if (u >= end) return;
     int b = 0, seq_begin = 0, len = 0;                              // the sequence of unit u, its first unit and its rows
-    for (int b0 = 0, before = 0;; b0 += 64) {
-        if (b0 > 0) len_of = b0 + lane < a.B ? length(b0 + lane) : 0;
-        const int n = len_of > 0 ? ((len_of + P::CH - 1) / P::CH + over) * HH : 0, upto = before + scan_wave(n);
-        const unsigned long long past = __ballot(upto > u);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            b = b0 + at;
-            seq_begin = __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(n, at);
-            len = __builtin_amdgcn_readlane(len_of, at);
-            break;
+    auto units_of = [&](int len) { return len > 0 ? (chunks_of(len) + over) * HH : 0; };
+    if (a.B <= 64) {
+        const int n = units_of(lengths.own), upto = scan_wave(n);
+        b = __builtin_ctzll(__ballot(upto > u));
+        seq_begin = __builtin_amdgcn_readlane(upto, b) - __builtin_amdgcn_readlane(n, b);
+        len = __builtin_amdgcn_readlane(lengths.own, b);
+    } else {
+        for (int b0 = 0, before = 0;; b0 += 512) {                  // a lane has eight sequences one after the other
+            int n = 0, lens[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lens[j] = length(min(b0 + lane * 8 + j, a.B - 1));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (b0 + lane * 8 + j >= a.B) lens[j] = 0;
+                n += units_of(lens[j]);
+            }
+            const int upto = before + scan_wave(n);
+            const unsigned long long past = __ballot(upto > u);
+            if (past) {
+                const int at = __builtin_ctzll(past);
+                seq_begin = __builtin_amdgcn_readlane(upto - n, at);
+                b = b0 + at * 8;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {                       // (the one that holds u, then no longer another)
+                    const int x = __builtin_amdgcn_readlane(lens[j], at), here = units_of(x);
+                    if (len == 0 && here > u - seq_begin) len = x;
+                    if (len == 0) { seq_begin += here; ++b; }
+                }
+                break;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
         }
-        before = __builtin_amdgcn_readlane(upto, 63);
     }
 
     const int block_shift = a.page_shift - (R == 8 ? 3 : 2), block_mask = (1 << block_shift) - 1;      // blocks of R rows
@@ -221,7 +261,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
     const bool out_whole = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_stride % 4 == 0;
 
     while (u < end) {
-        const int chunks = (len + P::CH - 1) / P::CH, per_head = chunks + over, hh = small_quotient(u - seq_begin, per_head), head_begin = seq_begin + hh * per_head;
+        const int chunks = chunks_of(len), per_head = chunks + over, hh = small_quotient(u - seq_begin, per_head), head_begin = seq_begin + hh * per_head;
         const int c0 = max(u - head_begin - over, 0), c1 = min(chunks, end - head_begin - over);
         const int next = min(end, head_begin + per_head);
         if (c1 <= 0) return;                                        // the run ends in what this one counts more
@@ -233,10 +273,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
         char* Vh = static_cast<char*>(a.v_pages) + kvh * head_bytes;
         // This wave's turns: rows first, first + CH, ... last, in a circle that begins at another place in every workgroup.  (Sequences whose pages lie a power of two apart, 64 pages
         // each, are at the same place of their memory channels in every row; workgroups that walk them in step meet there.)
-        const int first = c0 * P::CH + wave * P::TR, turns = c1 - c0 - ((c1 - 1) * P::CH + wave * P::TR >= len ? 1 : 0), last = first + (turns - 1) * P::CH;
+        const int row0 = WAVES ? 0 : wave * P::TR, first = c0 * CH + row0, turns = c1 - c0 - ((c1 - 1) * CH + row0 >= len ? 1 : 0), last = first + (turns - 1) * CH;
         int r = first;
-        if (turns >= 4) r += (run - small_quotient(run, turns) * turns) * P::CH;       // (a few turns do not meet for long)
-        auto after = [&](int row) { return row == last ? first : row + P::CH; };
+        if (turns >= 4) r += (run - small_quotient(run, turns) * turns) * CH;       // (a few turns do not meet for long)
+        auto after = [&](int row) { return row == last ? first : row + CH; };
 
         uint4 kr[U][KT][NK], vr[U][ND];
         // pages of the blocks of R rows that a lane loads of K and of V; blocks past the last are read as the last
@@ -269,7 +309,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             }
         };
         // the wave whose turn has the newest row rounds it as the pool does, and puts it into its page
-        const bool fresh = a.k_new && c1 == chunks && (newest / P::TR & 3) == wave;
+        const bool fresh = a.k_new && c1 == chunks && (WAVES || (newest / P::TR & 3) == wave);
         float m = -INFINITY, l = 0.f;
         f32x4 acc[ND];
 #pragma unroll
@@ -317,7 +357,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                     for (int e = 0; e < 2; ++e) {
                         const int d = lane + e * (HD / 2);
                         const T kt = held<T>(y[e]), vt = held<T>(z[e]);
-                        sh.new_k[d] = kt; sh.new_v[d] = vt;
+                        sh.new_k[wave][d] = kt; sh.new_v[wave][d] = vt;
                         if (h0 == 0 && present(new_page)) {
                             reinterpret_cast<T*>(Kh + new_page * page_bytes)[(newest & ((1 << a.page_shift) - 1)) * HD + d] = kt;
                             T rows[R];
@@ -389,7 +429,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         for (int t = 0; t < KT; ++t) {
                             if (r + x * RG + R * (i >> 2) + 4 * t + (i & 3) != newest) continue;
 #pragma unroll
-                            for (int k = 0; k < NK; ++k) __builtin_memcpy(&kr[x][t][k], &sh.new_k[k * 4 * QE + g * QE], 16);
+                            for (int k = 0; k < NK; ++k) __builtin_memcpy(&kr[x][t][k], &sh.new_k[wave][k * 4 * QE + g * QE], 16);
                         }
                 }
                 const uint4* q_at = q_lds;
@@ -480,7 +520,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
 #pragma unroll
                             for (int d = 0; d < ND; ++d) {
                                 uint32_t own = 0;
-                                __builtin_memcpy(&own, &sh.new_v[d * 16 + i], P::ES);
+                                __builtin_memcpy(&own, &sh.new_v[wave][d * 16 + i], P::ES);
                                 if (PER == 2) own |= own << 16;
                                 vr[x][d].x = (fresh_bits[0] & own) | (~fresh_bits[0] & vr[x][d].x);
                                 vr[x][d].y = (fresh_bits[1] & own) | (~fresh_bits[1] & vr[x][d].y);
@@ -531,12 +571,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
         asm volatile("" : "+s"(none));
         asm volatile("" : "+v"(still));
         const int H_ = H + none, HH_ = HH + none, GP_ = GP + none;
-        if (const int i = still & 15, g = (still & 63) >> 4; i < nh) {
+        if (const int i = still & 15, g = (still & 63) >> 4; !WAVES && i < nh) {
             if (g == 0) { sh.m[i][wave] = m; sh.l[i][wave] = l; }
 #pragma unroll
             for (int d = 0; d < ND; ++d) *reinterpret_cast<f32x4*>(&sh.o[wave][i][d * 16 + g * 4]) = acc[d];
         }
-        __syncthreads();
+        if (!WAVES) __syncthreads();
         // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
         int w0 = run, parts = 1;
         if (!whole) {
@@ -553,50 +593,76 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
             store_act4(a.out, b * a.out_stride + e, a.dtype, v, out_whole);
             if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H_ * HD), e, v, a.out_form.lo);
         };
-        // (32-bit offsets: the partial results of all runs are 16 MiB at most)
+        // (32-bit offsets: the partial results of all runs are 32 MiB at most)
         auto part_o_at = [&](unsigned slot, int h, int t) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_o) + ((slot * GP_ + h) * HD + t) * 4u); };
         auto part_ml_at = [&](unsigned slot, int h) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_ml) + (slot * GP_ + h) * 8u); };
-        auto publish = [&](unsigned slot, int h, int t, const float (&o)[4], float M, float L) {
+        auto publish_o = [&](unsigned slot, int h, int t, const float (&o)[4]) {
             st_agent2(part_o_at(slot, h, t), o[0], o[1]);
             st_agent2(part_o_at(slot, h, t + 2), o[2], o[3]);
-            if (t == 0) st_agent2(part_ml_at(slot, h), M, L);
         };
-        for (int idx = still; idx < items; idx += 256) {
-            const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
-            const f32x4 ms = *reinterpret_cast<const f32x4*>(sh.m[h]), ls = *reinterpret_cast<const f32x4*>(sh.l[h]);
-            f32x4 x[4];
+        auto publish_ml = [&](unsigned slot, int h, float M, float L) { st_agent2(part_ml_at(slot, h), M, L); };
+        if constexpr (!WAVES) {
+            for (int idx = still; idx < items; idx += 256) {
+                const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
+                const f32x4 ms = *reinterpret_cast<const f32x4*>(sh.m[h]), ls = *reinterpret_cast<const f32x4*>(sh.l[h]);
+                f32x4 x[4];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&sh.o[w][h][t]);
-            const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
-            float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&sh.o[w][h][t]);
+                const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3]));
+                float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const float f = ms[w] > -INFINITY ? __builtin_amdgcn_exp2f(ms[w] - M) : 0.f;
-                L += ls[w] * f;
+                for (int w = 0; w < 4; ++w) {
+                    const float f = ms[w] > -INFINITY ? __builtin_amdgcn_exp2f(ms[w] - M) : 0.f;
+                    L += ls[w] * f;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] += x[w][e] * f;
+                    for (int e = 0; e < 4; ++e) o[e] += x[w][e] * f;
+                }
+                if (whole) finish(h, t, o, L);
+                else {
+                    publish_o(slot_of(run - w0), h, t, o);
+                    if (t == 0) publish_ml(slot_of(run - w0), h, M, L);
+                }
             }
-            if (whole) finish(h, t, o, L); else publish(slot_of(run - w0), h, t, o, M, L);
+        } else if (const int i = still & 15, g = (still & 63) >> 4; i < nh) {       // a lane has the head, four dims of each tile
+#pragma unroll
+            for (int d = 0; d < ND; ++d) {
+                const float o[4] = {acc[d][0], acc[d][1], acc[d][2], acc[d][3]};
+                if (whole) finish(i, d * 16 + g * 4, o, l);
+                else publish_o(slot_of(run - w0), i, d * 16 + g * 4, o);
+            }
+            if (!whole && g == 0) publish_ml(slot_of(run - w0), i, m, l);
         }
-        if (!whole) {
-            constexpr int ITEMS = (kPagedHeads * (HD / 4) + 255) / 256;
+        auto join_all = [&](auto threads_) {
+            constexpr int THREADS = decltype(threads_)::value, ITEMS = kPagedHeads * (HD / 4) / THREADS, MOST = THREADS == 64 ? 5 : kJoin;
+            const int self = still & (THREADS - 1), column = THREADS == 64 ? wave : 0;
             // The run that arrives last joins them; more than kJoin in two rounds: the last of every kJoin joins these, the last of all joins what they give.
             auto arrive = [&](int* ticket, int of) {
                 wait_stores();
-                __syncthreads();
-                if (still == 0) {
-                    sh.is_last = atomicAdd(ticket, 1) == of - 1;
-                    if (sh.is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // all arrived: leave it clean
+                if constexpr (THREADS == 256) {
+                    __syncthreads();
+                    if (still == 0) {
+                        sh.is_last = atomicAdd(ticket, 1) == of - 1;
+                        if (sh.is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // all arrived: leave it clean
+                    }
+                    __syncthreads();
+                    return sh.is_last != 0;
+                } else {
+                    int is_last = 0;
+                    if (self == 0) {
+                        is_last = atomicAdd(ticket, 1) == of - 1;
+                        if (is_last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    }
+                    is_last = __builtin_amdgcn_readfirstlane(is_last);
+                    asm volatile("" ::: "memory");
+                    return is_last != 0;
                 }
-                __syncthreads();
-                return sh.is_last != 0;
             };
+            // done(h, t, o, M, L) of every item of this thread: four dims from t on of head h
             auto join = [&](auto flight, int first, int step, int count, auto done) {
                 constexpr int J = decltype(flight)::value;          // partial results in flight
-#pragma unroll
-                for (int it = 0; it < ITEMS; ++it) {
-                    const int idx = still + it * 256, h = idx / (HD / 4), t = idx % (HD / 4) * 4;
-                    if (idx >= items) break;
+                auto item = [&](int idx) {
+                    const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
+                    if (idx >= items) return;
                     float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
                     for (int k0 = 0; k0 < count; k0 += J) {
                         float2 ml[J], lo[J], hi[J];
@@ -625,40 +691,43 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
                         }
                         M = top;
                     }
-                    done(it, h, t, o, M, L);
+                    done(h, t, o, M, L);
+                };
+                if constexpr (THREADS == 256) {
+#pragma unroll
+                    for (int it = 0; it < ITEMS; ++it) item(self + it * 256);
+                } else {
+#pragma unroll 1
+                    for (int idx = self; idx < items; idx += 64) item(idx);
                 }
             };
             const int sets = (parts + kJoin - 1) / kJoin, first = (run - w0) / kJoin * kJoin, count = min(kJoin, parts - first);
             bool mine = true;
             if (sets > 1 && count > 1) {
                 mine = arrive(&a.tickets[a.B * HH_ + (int)slot_of(first)], count);
-                if (mine) {                                         // what they give goes into the first one's slot, once all threads have read it
-                    float js[ITEMS][6];
-                    join(std::integral_constant<int, kJoin>(), first, 1, count, [&](int it, int, int, const float (&o)[4], float M, float L) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) js[it][e] = o[e];
-                        js[it][4] = M; js[it][5] = L;
+                if (mine) {                                         // what they give goes into the first one's slot: a thread's dims as it has read them, maxima and sums once all have
+                    join(std::integral_constant<int, MOST>(), first, 1, count, [&](int h, int t, const float (&o)[4], float M, float L) {
+                        publish_o(slot_of(first), h, t, o);
+                        if (t == 0) { sh.m[h][column] = M; sh.l[h][column] = L; }
                     });
-                    __syncthreads();
-#pragma unroll
-                    for (int it = 0; it < ITEMS; ++it) {
-                        const int idx = still + it * 256;
-                        if (idx >= items) break;
-                        const float o[4] = {js[it][0], js[it][1], js[it][2], js[it][3]};
-                        publish(slot_of(first), idx / (HD / 4), idx % (HD / 4) * 4, o, js[it][4], js[it][5]);
-                    }
+                    if (THREADS == 256) __syncthreads();
+                    if (self < nh) publish_ml(slot_of(first), self, sh.m[self][column], sh.l[self][column]);
                 }
             }
             const int left = sets > 1 ? sets : parts;
             if (mine && arrive(&a.tickets[b * HH_ + hh], left)) {
-                auto last = [&](int, int h, int t, const float (&o)[4], float, float L) { finish(h, t, o, L); };
-                if (left <= 5) join(std::integral_constant<int, 5>(), 0, sets > 1 ? kJoin : 1, left, last);      // (640 rows, 32 heads)
-                else join(std::integral_constant<int, kJoin>(), 0, sets > 1 ? kJoin : 1, left, last);
+                auto last = [&](int h, int t, const float (&o)[4], float, float L) { finish(h, t, o, L); };
+                if (MOST > 5 && left <= 5) join(std::integral_constant<int, 5>(), 0, sets > 1 ? kJoin : 1, left, last);      // (640 rows, 32 heads)
+                else join(std::integral_constant<int, MOST>(), 0, sets > 1 ? kJoin : 1, left, last);
             }
+        };
+        if (!whole) {
+            if constexpr (WAVES) join_all(std::integral_constant<int, 64>());
+            else join_all(std::integral_constant<int, 256>());
         }
         u = next;
         if (u < end) {
-            __syncthreads();                                        // the merge has read what the next (sequence, heads) will write
+            if (!WAVES) __syncthreads();                            // the merge has read what the next (sequence, heads) will write
             if (u == seq_begin + per_head * HH) {                   // all heads of this sequence: the next one that has rows
                 seq_begin = u;
                 do len = __builtin_amdgcn_readfirstlane(length(++b)); while (len == 0);      // there is one: u < end <= total
@@ -667,15 +736,40 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
     }
 }
 
+// MANY: there are as many (sequence, heads) as waves, or nearly.  If those that have rows are as many, and have three chunks or less on average, every wave takes runs of its own: no merge of four,
+// no wave without rows where they are few, q prepared once instead of four times.  us a pass, runs of workgroups and of waves: 256 sequences of 30 / 100 / 200 / 500 rows of 8 KV heads, 32 query heads
+// 23.0 14.5 / 34.2 26.5 / 46.7 44.3 / 95.8 96.3; 128 x 100 rows of 32 heads 63.0 50.2; 512 x 64 of 8, 64 query heads 47.5 38.1; lengths of 1 to 2048, 256 x 8 KV heads, 32 query heads (2.6 chunks) 72.9 67.9.
+// Above that the few long sequences are shared by so many waves that it turns: 1 to 4096 (4.3 chunks) 106.3 111.3, 1 to 32768 with 64 query heads 517 556.  With fewer (sequence, heads) than waves every
+// wave has parts of them, to be joined: 7/8 as many, 200 rows, 64 query heads 47.6 55.1; 15/16 48.8 51.2, but 7/8 of 1 to 1000 rows, 32 query heads, 46.6 38.6.
+__host__ __device__ inline int nearly(int waves) { return waves - waves / 16; }
+
+template <typename T, int HD, typename A, bool MANY>
+__global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
+    __shared__ PagedShared<T, HD> sh;
+    paged_take_args(a);
+    auto length = [&](int b) { return min(max(a.rows[b], 0), a.max_rows); };
+    const Lengths n = take_lengths<PagedShape<T, HD>>(a.B, threadIdx.x & 63, length);
+    if constexpr (MANY) {
+        if (n.chunks <= 3 * n.live && n.live * a.H_kv * ((a.group + kPagedHeads - 1) / kPagedHeads) >= nearly((int)a.by_waves.d))
+            return attn_paged_runs<T, HD, A, true>(a, sh, n, length);
+    }
+    attn_paged_runs<T, HD, A, false>(a, sh, n, length);
+}
+
+template <typename T, int HD, bool MANY>
+int launch_many(const PagedAttnArgs& a, int n, hipStream_t s) {
+    if (a.dtype == D3_F32) hipLaunchKernelGGL((attn_paged_kernel<T, HD, float, MANY>), dim3(n), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((attn_paged_kernel<T, HD, uint16_t, MANY>), dim3(n), dim3(256), 0, s, a);
+    return (int)hipGetLastError();
+}
 template <typename T, int HD>
 int launch(PagedAttnArgs a, int n_cu, hipStream_t s) {
-    const long long most = (long long)a.B * a.H_kv * paged_head_tiles(a.group) * ((a.max_rows + PagedShape<T, HD>::CH - 1) / PagedShape<T, HD>::CH);
+    const long long heads = (long long)a.B * a.H_kv * paged_head_tiles(a.group), most = heads * ((a.max_rows + PagedShape<T, HD>::CH - 1) / PagedShape<T, HD>::CH);
     // as many workgroups as are resident, two per compute unit
-    const int n = (int)std::min<long long>(most, std::min(2 * n_cu, kPagedMaxWgs));
+    const int resident = std::min(2 * n_cu, kPagedMaxWgs), n = (int)std::min<long long>(most, resident);
     a.by_runs = Divisor(n);
-    if (a.dtype == D3_F32) hipLaunchKernelGGL((attn_paged_kernel<T, HD, float>), dim3(n), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((attn_paged_kernel<T, HD, uint16_t>), dim3(n), dim3(256), 0, s, a);
-    return (int)hipGetLastError();
+    a.by_waves = Divisor(4 * n);
+    return heads >= nearly(4 * resident) ? launch_many<T, HD, true>(a, n, s) : launch_many<T, HD, false>(a, n, s);
 }
 
 }  // namespace

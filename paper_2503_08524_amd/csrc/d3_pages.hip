@@ -30,8 +30,8 @@ int check_desc(const d3_pages_desc* d) {
     if (d->max_batch < 1 || d->max_batch > kPagesMaxSeqs) return fail(D3_ESHAPE, "pages: max_batch must be in [1, %d] (got %d)", kPagesMaxSeqs, d->max_batch);
     if (d->max_pages < 1 || (int64_t)d->max_pages * d->page_rows > kMostTokens || (int64_t)d->max_pages * d->max_batch > INT32_MAX)
         return fail(D3_ESHAPE, "pages: max_pages must be positive, max_pages * page_rows at most 2^30 and max_pages * max_batch below 2^31 (got %d)", d->max_pages);
-    // the attention counts its chunks of work in 32 bits
-    const int64_t chunks = ((int64_t)d->max_pages * d->page_rows + paged_chunk_rows(d->head_dim, d->kv_dtype) - 1) / paged_chunk_rows(d->head_dim, d->kv_dtype);
+    // the attention counts its pieces of work in 32 bits
+    const int64_t chunks = ((int64_t)d->max_pages * d->page_rows + paged_turn_rows(d->head_dim, d->kv_dtype) - 1) / paged_turn_rows(d->head_dim, d->kv_dtype);
     const int64_t per_chunk = (int64_t)d->n_kv_heads * paged_head_tiles(d->n_heads / d->n_kv_heads) * d->max_batch;
     if (chunks + kPagedOverhead > INT32_MAX / per_chunk)
         return fail(D3_ESHAPE, "pages: %d sequences of up to %d pages are more rows than one attention launch counts", d->max_batch, d->max_pages);
@@ -41,10 +41,10 @@ int check_desc(const d3_pages_desc* d) {
 // offsets behind the partial outputs; returns the whole size
 size_t layout(const d3_pages_desc& d, size_t* part_ml, size_t* tickets) {
     const int group = d.n_heads / d.n_kv_heads;
-    const size_t partials = 2 * (size_t)kPagedMaxWgs * (group < kPagedHeads ? group : kPagedHeads);
+    const size_t partials = 2 * (size_t)kPagedMaxRuns * (group < kPagedHeads ? group : kPagedHeads);
     *part_ml = align_up(partials * d.head_dim * 4);
     *tickets = *part_ml + align_up(partials * 2 * 4);
-    return *tickets + align_up(((size_t)d.max_batch * d.n_kv_heads * paged_head_tiles(group) + 2 * kPagedMaxWgs) * 4);
+    return *tickets + align_up(((size_t)d.max_batch * d.n_kv_heads * paged_head_tiles(group) + 2 * kPagedMaxRuns) * 4);
 }
 
 int check_layers(const d3_pages* p, const char* who, int32_t layer, int32_t n) {

@@ -12,7 +12,8 @@ namespace d3 {
 
 constexpr int kPagesMaxSeqs = 4096;        // sequences of a call
 constexpr int kPagedHeads = 16;            // query heads of one workgroup: the columns of a matrix instruction
-constexpr int kPagedMaxWgs = 1024;         // workgroups of an attention launch
+constexpr int kPagedMaxWgs = 512;          // workgroups of an attention launch, four waves each
+constexpr int kPagedMaxRuns = 4 * kPagedMaxWgs;
 constexpr int kPagedOverhead = 1;          // what beginning and ending a (sequence, heads) costs a workgroup, in chunks
 
 // As a pool holds a value.
@@ -63,13 +64,13 @@ struct PagedAttnArgs {
     void* out;
     bf16_t* out_split;                     // optional split copy
     SplitForm out_form;
-    float *part_o, *part_ml;               // [2 * workgroups][min(group, 16)][hd], [..][2]
-    int* tickets;                          // [B][H_kv * tiles], then [2 * workgroups], zero between launches
-    Divisor by_runs;                       // set by launch_attention_paged: its workgroups
+    float *part_o, *part_ml;               // [2 * runs][min(group, 16)][hd], [..][2]
+    int* tickets;                          // [B][H_kv * tiles], then [2 * runs], zero between launches
+    Divisor by_runs, by_waves;             // set by launch_attention_paged: its workgroups and their waves
 };
 int launch_attention_paged(const PagedAttnArgs& a, int hd, int kv_dtype, int n_cu, hipStream_t s);
-// rows of a workgroup's turn: 4 waves, 16 loads of 16 bytes a lane
-inline int paged_chunk_rows(int hd, int kv_dtype) { return 4 * 16 * 64 * 16 / (2 * hd * kv_elem_bytes(kv_dtype)); }
+// rows of a wave's turn: 16 loads of 16 bytes a lane
+inline int paged_turn_rows(int hd, int kv_dtype) { return 16 * 64 * 16 / (2 * hd * kv_elem_bytes(kv_dtype)); }
 inline int paged_head_tiles(int group) { return (group + kPagedHeads - 1) / kPagedHeads; }
 
 }  // namespace d3

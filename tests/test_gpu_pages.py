@@ -200,6 +200,38 @@ def test_attention_runs_of_many_chunks(heads, group, hd, kv, act, page_rows, ord
     _check(out, *_reference(cache, q.double(), lens))
 
 
+@pytest.mark.parametrize("B,heads,group,hd,kv,act,page_rows,longest,long", [
+    (300, 8, 4, 128, "f16", "bf16", 16, 70, 4000), (70, 32, 1, 128, "f16", "f32", 16, 100, 0), (260, 4, 17, 128, "f16", "f32", 32, 100, 1000),
+    (270, 8, 2, 128, "f32", "f32", 16, 50, 2000), (150, 16, 3, 64, "f16", "f16", 16, 200, 6000), (520, 4, 16, 64, "f32", "bf16", 64, 90, 3000)])
+def test_attention_of_many_short_sequences(B, heads, group, hd, kv, act, page_rows, longest, long):
+    """As many (sequence, heads) as waves, and few rows of each: every wave takes a run of its own.  Also with sequences that many waves share, and with the same tables when half of
+    the sequences have no rows, or all have more of them."""
+    import torch
+    turn = 1024 * 8 // (hd * (2 if kv == "f16" else 4))             # rows of a wave's turn
+    rng = np.random.RandomState(B)
+    few = rng.randint(1, longest, B)
+    few[:6] = 1, turn, turn + 1, 2 * turn, turn - 1, 0
+    few[B // 2] = long or 1
+    few[B // 3] = 0
+    many = np.maximum(few, 4 * 4 * turn + rng.randint(-3, 4, B))    # four turns of four waves
+    half = np.where(np.arange(B) % 2 == 0, few, 0)
+    cache, g = _cache(many.tolist(), heads, group, hd, kv, page_rows, seed=B)
+    q = torch.empty(B, heads * group, hd, dtype=_types()[act], device=DEV).normal_(generator=g)
+    k, v = (torch.empty(B, heads, hd, dtype=_types()[act], device=DEV).normal_(generator=g) for _ in range(2))
+    cs = _angles(list(range(B)), hd)
+    for lens in (few, half, many, few):
+        lens = lens.tolist()
+        cache.rows.copy_(torch.tensor(lens, dtype=torch.int32))
+        out = cache.attend(0, q, k, v, rope_cs=cs)
+        live = [b for b in range(B) if lens[b]]
+        at = torch.cat([_slots(cache, b, [lens[b] - 1]) for b in live])
+        for pool, x in ((cache.k_pages, _turned(k.double(), cs)), (cache.v_pages, v.double())):
+            err = (_as_rows(cache, pool)[0, at].double() - x[live]).abs()
+            assert (err <= torch.finfo(pool.dtype).eps / 2 * x[live].abs() + 3 * 2.0 ** -24 * x[live].abs().amax() * 2 + 2.0 ** -25).all()
+        _check(out, *_reference(cache, _turned(q.double(), cs), lens))
+        assert torch.equal(out, cache.attend(0, q, k, v, rope_cs=cs))
+
+
 def test_attention_of_thousands_of_sequences():
     import torch
     lens = [(b * 7919) % 23 if b % 3 else 0 for b in range(4096)]
