@@ -274,7 +274,7 @@ int d3_pages_reserve(d3_pages *pages, int32_t B, const int32_t *added, const int
 /* Keys and values of n tokens into their slots of `n_layers` layers from `layer` on.  k, v: dev [n_layers][n][H_kv][head_dim] of `dtype` (any of d3_dtype),
  * element (l, t, h, e) at l * layer_stride + t * token_stride + h * head_stride + e (strides in elements, multiples of 16 bytes; pointers 16-byte aligned, rope_cs too).  rope_cs: dev float
  * [n][head_dim / 2][2], (cos, sin) of each token's angles, or NULL: keys turn by it (dims j and j + head_dim / 2 by angle j) before they are rounded once to the
- * pool's type. */
+ * pool's type.  n at most 2^28. */
 int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t *slots, const void *k, const void *v, int32_t dtype,
                     int64_t token_stride, int64_t head_stride, int64_t layer_stride, const float *rope_cs, void *hip_stream);
 
@@ -288,7 +288,7 @@ int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q,
                        int64_t out_stride, void *hip_stream);
 
 /* The missing-state fill on pages (D3_FILL_COPY, Section 3.2): rows `slots` of layer `src` are copied into layers [first, first + n_layers), which
- * must not hold src; src < 0: zeros. */
+ * must not hold src; src < 0: zeros.  n * H_kv at most 2^25. */
 int d3_pages_fill(d3_pages *pages, int32_t n, const int32_t *slots, int32_t src, int32_t first, int32_t n_layers, void *hip_stream);
 
 /* Rows [row_begin, row_begin + n) of sequence `seq` of the context's own cache (counted from the sequence's first row if the batch was left-padded) into

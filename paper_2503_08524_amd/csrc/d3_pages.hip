@@ -12,6 +12,8 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int kMostTokens = 1 << 30;       // rows of one call
+// a launch has fewer than 2^32 threads: an append has 8 a row and head (of the heads' own grid dimension), a fill 64 a row and head
+constexpr int kMostAppendTokens = 1 << 28, kMostFillHeads = 1 << 25;
 
 size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 int elem_bytes(int dtype) { return dtype == D3_F32 ? 4 : 2; }
@@ -154,6 +156,7 @@ extern "C" int d3_pages_append(d3_pages* pages, int32_t layer, int32_t n_layers,
     D3_CHECK(check_tokens("d3_pages_append", n));
     D3_CHECK(check_layers(pages, "d3_pages_append", layer, n_layers));
     D3_CHECK(check_dtype("d3_pages_append", dtype));
+    if (n > kMostAppendTokens) return fail(D3_ESHAPE, "d3_pages_append: %d rows are more than one launch counts (%d)", n, kMostAppendTokens);
     if (n == 0) return D3_OK;
     if (!slots || !k || !v) return fail(D3_EINVAL, "d3_pages_append: NULL argument");
     const int unit = 16 / elem_bytes(dtype);
@@ -205,7 +208,7 @@ extern "C" int d3_pages_fill(d3_pages* pages, int32_t n, const int32_t* slots, i
     if (src >= pages->desc.n_layers || (src >= first && src < first + n_layers))
         return fail(D3_ERANGE, "d3_pages_fill: source layer %d must be one of the pool's and outside [%d, %d)", src, first, first + n_layers);
     if (!slots) return fail(D3_EINVAL, "d3_pages_fill: NULL argument");
-    if ((int64_t)n * pages->desc.n_kv_heads > INT32_MAX) return fail(D3_ESHAPE, "d3_pages_fill: %d rows of %d heads are more than one launch counts", n, pages->desc.n_kv_heads);
+    if ((int64_t)n * pages->desc.n_kv_heads > kMostFillHeads) return fail(D3_ESHAPE, "d3_pages_fill: %d rows of %d KV heads are more than one launch counts (%d heads of rows)", n, pages->desc.n_kv_heads, kMostFillHeads);
     const d3_pages_desc& d = pages->desc;
     PagesFillArgs a{};
     a.n = n; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_shift = __builtin_ctz(d.page_rows); a.by_heads = Divisor(d.n_kv_heads); a.first = first; a.n_layers = n_layers; a.src = src < 0 ? -1 : src;

@@ -689,3 +689,19 @@ def test_refusals():
             call()
         assert e.value.status == status and word in str(e.value)
     assert not cache.k_pages.any() and not cache.v_pages.any()
+
+
+def test_more_rows_than_a_launch_counts_are_refused():
+    """Refused before the slots are looked at (there are three)."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    cache = PagedCache(4, 2, 64, 8, 16, 3, 4, n_layers=2, device=DEV)
+    slots, k = torch.zeros(3, dtype=torch.int32, device=DEV), torch.zeros(3, 2, 64, device=DEV)
+    for n, status, word in (((1 << 28) + 1, -2, "more than one launch"), ((1 << 30) + 1, -1, "2^30"), (-1, -1, "2^30")):
+        assert cache.lib.d3_pages_append(cache.handle, 0, 1, n, slots.data_ptr(), k.data_ptr(), k.data_ptr(), 0, 0, 64, 0, None, None) == status
+        assert word in cache.lib.d3_last_error().decode()
+    for n, status, word in (((1 << 24) + 1, -2, "more than one launch"), (1 << 30, -2, "more than one launch"), ((1 << 30) + 1, -1, "2^30")):
+        assert cache.lib.d3_pages_fill(cache.handle, n, slots.data_ptr(), 0, 1, 1, None) == status
+        assert word in cache.lib.d3_last_error().decode()
+    assert cache.lib.d3_pages_fill(cache.handle, (1 << 30) + 1, None, 0, 1, 1, None) == -1
+    torch.cuda.synchronize()
