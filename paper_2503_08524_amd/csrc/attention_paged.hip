@@ -55,6 +55,7 @@ struct __align__(16) PagedShared {
 };
 
 constexpr int kJoin = 16;      // partial results that one workgroup joins at a time, all of their loads in flight together
+constexpr int kAgent = 16;     // buffer accesses at agent scope (past the XCD's own L2, like st_agent and ld_agent)
 
 // Activations as they lie in memory (A: float, or the bits of a 16-bit type) and as fp32.  The two are apart so that all loads are requested before the first conversion waits.
 template <int N, typename A>
@@ -593,12 +594,11 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
             store_act4(a.out, b * a.out_stride + e, a.dtype, v, out_whole);
             if (a.out_split) store_split4(a.out_split + b * a.out_form.pitch(H_ * HD), e, v, a.out_form.lo);
         };
-        // (32-bit offsets: the partial results of all runs are 32 MiB at most)
-        auto part_o_at = [&](unsigned slot, int h, int t) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_o) + ((slot * GP_ + h) * HD + t) * 4u); };
+        // 16 bytes an access (two of 8, a head at a time: 64 x 1000 rows of one KV head, 16 query heads, 19.1 us; so 15.6); 32-bit offsets, the partial results of all runs are 32 MiB at most
+        const auto part_buf = __builtin_amdgcn_make_buffer_rsrc(a.part_o + none, 0, 2 * by_runs.d * GP_ * (HD * 4), 0x00027000);
         auto part_ml_at = [&](unsigned slot, int h) { return reinterpret_cast<float*>(reinterpret_cast<char*>(a.part_ml) + (slot * GP_ + h) * 8u); };
         auto publish_o = [&](unsigned slot, int h, int t, const float (&o)[4]) {
-            st_agent2(part_o_at(slot, h, t), o[0], o[1]);
-            st_agent2(part_o_at(slot, h, t + 2), o[2], o[3]);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{o[0], o[1], o[2], o[3]}), part_buf, (h * HD + t) * 4, slot * GP_ * (HD * 4), kAgent);
         };
         auto publish_ml = [&](unsigned slot, int h, float M, float L) { st_agent2(part_ml_at(slot, h), M, L); };
         if constexpr (!WAVES) {
@@ -633,7 +633,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
             if (!whole && g == 0) publish_ml(slot_of(run - w0), i, m, l);
         }
         auto join_all = [&](auto threads_) {
-            constexpr int THREADS = decltype(threads_)::value, ITEMS = kPagedHeads * (HD / 4) / THREADS, MOST = THREADS == 64 ? 5 : kJoin;
+            constexpr int THREADS = decltype(threads_)::value, ITEMS = kPagedHeads * (HD / 4) / THREADS;
             const int self = still & (THREADS - 1), column = THREADS == 64 ? wave : 0;
             // The run that arrives last joins them; more than kJoin in two rounds: the last of every kJoin joins these, the last of all joins what they give.
             auto arrive = [&](int* ticket, int of) {
@@ -657,56 +657,76 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                     return is_last != 0;
                 }
             };
-            // done(h, t, o, M, L) of every item of this thread: four dims from t on of head h
-            auto join = [&](auto flight, int first, int step, int count, auto done) {
-                constexpr int J = decltype(flight)::value;          // partial results in flight
-                auto item = [&](int idx) {
-                    const int h = idx / (HD / 4), t = idx % (HD / 4) * 4;
-                    if (idx >= items) return;
-                    float M = -INFINITY, L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+            // done(h, t, o, M, L) of every item of this thread, four dims from t on of head h: J partial results of N items in flight
+            auto join = [&](auto flight, auto items_at_once, int first, int step, int count, auto done) {
+                constexpr int J = decltype(flight)::value, N = decltype(items_at_once)::value;
+                auto some = [&](int begin) {
+                    int at[N], h[N];
+                    float M[N], L[N], o[N][4];
+#pragma unroll
+                    for (int n = 0; n < N; ++n) {
+                        const int idx = min(begin + n * THREADS, items - 1);
+                        h[n] = idx / (HD / 4); at[n] = idx * 16;
+                        M[n] = -INFINITY; L[n] = o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+                    }
                     for (int k0 = 0; k0 < count; k0 += J) {
-                        float2 ml[J], lo[J], hi[J];
+                        float2 ml[N][J];
+                        f32x4 x[N][J];
 #pragma unroll
                         for (int k = 0; k < J; ++k) {
                             const unsigned slot = slot_of(first + min(k0 + k, count - 1) * step);
-                            ml[k] = ld_agent2(part_ml_at(slot, h));
-                            lo[k] = ld_agent2(part_o_at(slot, h, t));
-                            hi[k] = ld_agent2(part_o_at(slot, h, t + 2));
-                        }
-                        float top = M;
 #pragma unroll
-                        for (int k = 0; k < J; ++k) {
-                            if (k0 + k >= count) { ml[k] = make_float2(-INFINITY, 0.f); lo[k] = hi[k] = make_float2(0.f, 0.f); }
-                            top = fmaxf(top, ml[k].x);
+                            for (int n = 0; n < N; ++n) {
+                                ml[n][k] = ld_agent2(part_ml_at(slot, h[n]));
+                                x[n][k] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(part_buf, at[n], slot * GP_ * (HD * 4), kAgent));
+                            }
                         }
-                        const float keep = M > -INFINITY ? __builtin_amdgcn_exp2f(M - top) : 0.f;
-                        L *= keep;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] *= keep;
+                        for (int n = 0; n < N; ++n) {
+                            float top = M[n];
 #pragma unroll
-                        for (int k = 0; k < J; ++k) {
-                            const float f = ml[k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[k].x - top) : 0.f;
-                            L += ml[k].y * f;
-                            o[0] += lo[k].x * f; o[1] += lo[k].y * f; o[2] += hi[k].x * f; o[3] += hi[k].y * f;
+                            for (int k = 0; k < J; ++k) {
+                                if (k0 + k >= count) { ml[n][k] = make_float2(-INFINITY, 0.f); x[n][k] = f32x4{0.f, 0.f, 0.f, 0.f}; }
+                                top = fmaxf(top, ml[n][k].x);
+                            }
+                            const float keep = M[n] > -INFINITY ? __builtin_amdgcn_exp2f(M[n] - top) : 0.f;
+                            L[n] *= keep;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[n][e] *= keep;
+#pragma unroll
+                            for (int k = 0; k < J; ++k) {
+                                const float f = ml[n][k].x > -INFINITY ? __builtin_amdgcn_exp2f(ml[n][k].x - top) : 0.f;
+                                L[n] += ml[n][k].y * f;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[n][e] += x[n][k][e] * f;
+                            }
+                            M[n] = top;
                         }
-                        M = top;
                     }
-                    done(h, t, o, M, L);
-                };
-                if constexpr (THREADS == 256) {
 #pragma unroll
-                    for (int it = 0; it < ITEMS; ++it) item(self + it * 256);
+                    for (int n = 0; n < N; ++n) if (begin + n * THREADS < items) done(h[n], at[n] / 4 % HD, o[n], M[n], L[n]);
+                };
+                if constexpr (THREADS == 256) {                     // N is all there are
+                    if (self < items) some(self);
                 } else {
 #pragma unroll 1
-                    for (int idx = self; idx < items; idx += 64) item(idx);
+                    for (int idx = self; idx < items; idx += 64) some(idx);
                 }
+            };
+            auto join_some = [&](int first, int step, int count, auto done) {
+                typedef std::integral_constant<int, 1> One;
+                typedef std::integral_constant<int, 5> Five;
+                if constexpr (THREADS == 64) join(Five(), One(), first, step, count, done);
+                else if (ITEMS > 1 && items > THREADS) join(std::integral_constant<int, 8>(), std::integral_constant<int, 2>(), first, step, count, done);
+                else if (count <= 5) join(Five(), One(), first, step, count, done);      // (640 rows, 32 heads)
+                else join(std::integral_constant<int, kJoin>(), One(), first, step, count, done);
             };
             const int sets = (parts + kJoin - 1) / kJoin, first = (run - w0) / kJoin * kJoin, count = min(kJoin, parts - first);
             bool mine = true;
             if (sets > 1 && count > 1) {
                 mine = arrive(&a.tickets[a.B * HH_ + (int)slot_of(first)], count);
                 if (mine) {                                         // what they give goes into the first one's slot: a thread's dims as it has read them, maxima and sums once all have
-                    join(std::integral_constant<int, MOST>(), first, 1, count, [&](int h, int t, const float (&o)[4], float M, float L) {
+                    join_some(first, 1, count, [&](int h, int t, const float (&o)[4], float M, float L) {
                         publish_o(slot_of(first), h, t, o);
                         if (t == 0) { sh.m[h][column] = M; sh.l[h][column] = L; }
                     });
@@ -717,8 +737,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
             const int left = sets > 1 ? sets : parts;
             if (mine && arrive(&a.tickets[b * HH_ + hh], left)) {
                 auto last = [&](int h, int t, const float (&o)[4], float, float L) { finish(h, t, o, L); };
-                if (MOST > 5 && left <= 5) join(std::integral_constant<int, 5>(), 0, sets > 1 ? kJoin : 1, left, last);      // (640 rows, 32 heads)
-                else join(std::integral_constant<int, MOST>(), 0, sets > 1 ? kJoin : 1, left, last);
+                join_some(0, sets > 1 ? kJoin : 1, left, last);
             }
         };
         if (!whole) {
