@@ -616,6 +616,38 @@ def test_a_captured_step_replayed_while_sequences_grow():
     assert caches[0].rows.tolist() == [55, 26, 225]
 
 
+def test_a_captured_attention_whose_runs_become_those_of_waves_and_of_workgroups():
+    """One launch of 300 sequences, replayed while their lengths change: few rows each (runs of waves), half of them idle, one of them long, many rows each (runs of workgroups), none."""
+    import torch
+    rng = np.random.RandomState(5)
+    B, heads = 300, 8
+    few = rng.randint(1, 60, B)
+    one = few.copy()
+    one[77] = 3000
+    many = rng.randint(500, 700, B)
+    cache, g = _cache(np.maximum(many, one).tolist(), heads, 2, 64, "f16", 16, seed=3)
+    q = torch.empty(B, heads * 2, 64, device=DEV).normal_(generator=g)
+    k, v = (torch.empty(B, heads, 64, device=DEV).normal_(generator=g) for _ in range(2))
+    cases = [torch.tensor(x, dtype=torch.int32, device=DEV) for x in (few, np.where(np.arange(B) % 2, few, 0), one, many, np.zeros(B), few)]
+    for _ in range(2):                                              # (the newest row of one length is an older row of a longer one: all are written first)
+        want = []
+        for lens in cases:
+            cache.rows.copy_(lens)
+            want.append(cache.attend(0, q, k, v))
+    out = torch.empty_like(q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        cache.attend(0, q, k, v, out=out)
+    for _ in range(3):
+        for lens, expected in zip(cases, want):
+            cache.rows.copy_(lens)
+            out.fill_(math.nan)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, expected)
+    _check(want[2], *_reference(cache, q.double(), one.tolist()))
+
+
 def test_calls_on_another_stream():
     import torch
     cache, g = _cache([100, 5], 2, 2, 128, "f16", 16, seed=11, room=1)
