@@ -278,9 +278,14 @@ int d3_pages_reserve(d3_pages *pages, int32_t B, const int32_t *added, const int
 int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t *slots, const void *k, const void *v, int32_t dtype,
                     int64_t token_stride, int64_t head_stride, int64_t layer_stride, const float *rope_cs, void *hip_stream);
 
+/* The rows of the sequences that a reserve gave some, 0 for the others (refused, paused, ended): live[b] = starts[b] == starts[b + 1] ? 0 : rows[b], b < B, all dev int32, starts as
+ * d3_pages_reserve wrote it.  As `rows` of d3_pages_attention it leaves the others out: nothing of them is read or written but their out, which is 0. */
+int d3_pages_live(d3_pages *pages, int32_t B, const int32_t *rows, const int32_t *starts, int32_t *live, void *hip_stream);
+
 /* Attention of one token per sequence over its pages: out[b][h] = softmax(scale * q[b][h] . K^T) V over rows [0, rows[b]) of sequence b; 0 where it has no row.
  * q, out: dev [B][n_heads][head_dim] of `dtype`, sequence b at b * q_stride, b * out_stride.  k_new, v_new: dev [B][H_kv][head_dim] of `dtype` at b * kv_stride, or both NULL.
- * Given, they are row rows[b] - 1, which the call also writes to its page (which no other sequence of the call may list); else that row is there already.  rope_cs: dev float [B][head_dim / 2][2]: q and
+ * Given, they are row rows[b] - 1 of every sequence that has rows, which the call also writes to its page (which no other sequence of the call may list); else that row is there already.
+ * The call cannot tell a sequence that a reserve refused, or that asked for nothing: it would lose its newest row, so `rows` is then d3_pages_live's.  rope_cs: dev float [B][head_dim / 2][2]: q and
  * k_new turn by it; NULL: neither does.  q, k_new, v_new, rope_cs 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
  * out may be q itself.  Keys and values are used as the pool holds them; sums and softmax in 32 bits. */
 int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,
@@ -296,11 +301,18 @@ int d3_pages_fill(d3_pages *pages, int32_t n, const int32_t *slots, int32_t src,
 int d3_store_pages(d3_ctx *ctx, d3_pages *pages, int32_t seq, int32_t row_begin, int32_t n, const int32_t *slots, void *hip_stream);
 
 /* One decode step (as d3_decode_step) of B sequences whose rows are in `pages`: sequence b's token is row rows[b] - 1, for which d3_pages_reserve has made
- * room, and its rotary position; a sequence without rows is idle (its tok_out and logits mean nothing).  Runs the blocks of step `step_i` of the plan, 0 <= step_i < n_steps, in any order
+ * room, and its rotary position; a sequence without rows is idle (tok_out[b] = tok_in[b], its logits and hidden_dump mean nothing).  Only for callers who know that every sequence with rows has got
+ * one: of a sequence that was refused or asked for none the step would overwrite the newest row (d3_decode_step_granted leaves it as it is).  Runs the blocks of step `step_i` of the plan, 0 <= step_i < n_steps, in any order
  * of steps; the context's own cache, row count and step counter stay as they are.  D3_ESHAPE unless the pages have the context's shape and cache type;
  * D3_ESTATE with D3_FILL_RECOMPUTE. */
 int d3_decode_step_paged(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, int32_t B, int32_t step_i, const int32_t *tables,
                          const int32_t *rows, int32_t *tok_out, float *logits, float *hidden_dump, void *hip_stream);
+
+/* d3_decode_step_paged of the sequences that the reserve before it gave a row to.  starts: dev int32 [B + 1] of that d3_pages_reserve, in which every sequence that takes part has
+ * asked for one row: where starts[b] == starts[b + 1] (refused, paused, ended) sequence b is idle, its pages and tables are not read or written.  So a sequence that was refused goes on with the same token once its request is granted, with tok_out = tok_in and reserve and step
+ * in one captured graph too, and sequences of different ages take their steps one group after the other: a reserve and a step, of its own step_i, for each. */
+int d3_decode_step_granted(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, int32_t B, int32_t step_i, const int32_t *tables, const int32_t *rows,
+                           const int32_t *starts, int32_t *tok_out, float *logits, float *hidden_dump, void *hip_stream);
 
 /* d3_pages_fill of the blocks that step `step_i` of the context's plan drops, from the block d3_fill_missing_kv takes (Section 3.2). */
 int d3_fill_missing_paged(d3_ctx *ctx, d3_pages *pages, int32_t step_i, int32_t n, const int32_t *slots, void *hip_stream);

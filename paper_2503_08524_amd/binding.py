@@ -88,9 +88,11 @@ def load_library() -> C.CDLL:
         lib.d3_pages_reserve.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
         lib.d3_pages_append.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, i64, i64, i64, vp, vp]
         lib.d3_pages_attention.argtypes = [vp, i32, i32, vp, vp, vp, i32, i64, i64, vp, vp, vp, C.c_float, vp, i64, vp]
+        lib.d3_pages_live.argtypes = [vp, i32, vp, vp, vp, vp]
         lib.d3_pages_fill.argtypes = [vp, i32, vp, i32, i32, i32, vp]
         lib.d3_store_pages.argtypes = [vp, vp, i32, i32, i32, vp, vp]
         lib.d3_decode_step_paged.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+        lib.d3_decode_step_granted.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
         lib.d3_fill_missing_paged.argtypes = [vp, vp, i32, i32, vp, vp]
         lib.d3_mfma_yardstick.argtypes = [vp, i32, i32, vp]
         lib.d3_profile_select.argtypes = [vp, i32]
@@ -258,13 +260,20 @@ class Decoder:
         cache._ints(slots=slots)
         _check(self.lib.d3_store_pages(self.ctx, cache.handle, seq, row_begin, slots.numel(), slots.data_ptr(), self._stream()))
 
-    def decode_step_paged(self, cache: "PagedCache", tok_in, step_i: int, tok_out, logits=None, hidden_dump=None) -> None:
-        """One step of the cache's first tok_in.numel() sequences, whose newest rows cache.reserve has made room for."""
+    def decode_step_paged(self, cache: "PagedCache", tok_in, step_i: int, tok_out, logits=None, hidden_dump=None, starts=None) -> None:
+        """One step of the cache's first tok_in.numel() sequences, whose newest rows cache.reserve has made room for.  starts: what that reserve returned; the sequences
+        that it gave no row (refused, paused, ended) are idle: their rows stay, tok_out is tok_in.  Without it every sequence that has rows must have got one, or
+        the step overwrites its newest row."""
         cache._ints(tok_in=tok_in, tok_out=tok_out)
-        if tok_out.numel() < tok_in.numel():
+        B = tok_in.numel()
+        if tok_out.numel() < B:
             raise ValueError("tok_out is shorter than tok_in")
-        _check(self.lib.d3_decode_step_paged(self.ctx, cache.handle, tok_in.data_ptr(), tok_in.numel(), step_i, cache.tables.data_ptr(),
-                                             cache.rows.data_ptr(), tok_out.data_ptr(), _ptr(logits), _ptr(hidden_dump), self._stream()))
+        at = (self.ctx, cache.handle, tok_in.data_ptr(), B, step_i, cache.tables.data_ptr(), cache.rows.data_ptr())
+        out = (tok_out.data_ptr(), _ptr(logits), _ptr(hidden_dump), self._stream())
+        if starts is None:
+            _check(self.lib.d3_decode_step_paged(*at, *out))
+        else:
+            _check(self.lib.d3_decode_step_granted(*at, cache._starts(starts, B), *out))
 
     def fill_missing_paged(self, cache: "PagedCache", slots, step_i: int) -> None:
         """COPY fill of the rows `slots` in the blocks that step step_i of the plan drops."""
@@ -351,6 +360,7 @@ class PagedCache:
             self.n_free = buffer("n_free", n_free, (2,), torch.int32, torch.zeros)
             if n_free is None:
                 self.n_free[:1].fill_(n_pages)
+            self._live = torch.empty(max_batch, dtype=torch.int32, device=self.device)      # rows that an attend with starts counts
             self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
             handle = C.c_void_p()
             _check(self.lib.d3_pages_create(C.byref(handle), C.byref(desc), self.k_pages.data_ptr(), self.v_pages.data_ptr(),
@@ -372,6 +382,12 @@ class PagedCache:
         for name, t in tensors.items():
             if t.dtype is not self._int32 or t.get_device() != self._index or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous int32 tensor on {self.device}")
+
+    def _starts(self, starts, B: int) -> int:
+        self._ints(starts=starts)
+        if starts.numel() < B + 1:
+            raise ValueError(f"starts must have {B + 1} entries, as reserve returns it for these sequences")
+        return starts.data_ptr()
 
     def _angles(self, rope_cs, n: int) -> Optional[int]:
         if rope_cs is None:
@@ -426,10 +442,12 @@ class PagedCache:
         _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, strides[-3], strides[-2],
                                         strides[0] if len(strides) == 4 else 0, self._angles(rope_cs, n), self._stream()))
 
-    def attend(self, layer: int, q, k=None, v=None, rope_cs=None, scale: float = 0.0, out=None):
+    def attend(self, layer: int, q, k=None, v=None, rope_cs=None, scale: float = 0.0, out=None, starts=None):
         """Attention of one token of each of the first B sequences, q [B][n_heads][head_dim], over their rows; returns out [B][n_heads][head_dim] of q's dtype.
         k, v [B][n_kv_heads][head_dim]: the newest rows (row rows[b] - 1), which the call also writes to their pages; without them they are there already.
-        rope_cs [B][head_dim / 2][2]: q and k turn by it.  scale 0: 1 / sqrt(head_dim)."""
+        rope_cs [B][head_dim / 2][2]: q and k turn by it.  scale 0: 1 / sqrt(head_dim).
+        starts: what the reserve before it returned; of the sequences that it gave no row nothing is read or written, and out is 0.  Without it, and with k and v, every sequence
+        that has rows must have got one."""
         B, dtype, kind = q.shape[0], q.dtype, self._kind(q)
         dims = (B, self.n_heads, self.head_dim)
         if out is None:
@@ -448,8 +466,12 @@ class PagedCache:
             k_at, v_at = k.data_ptr(), v.data_ptr()
         elif k is not None or v is not None:
             raise ValueError("k and v come together or not at all")
-        _check(self.lib.d3_pages_attention(self.handle, layer, B, q.data_ptr(), k_at, v_at, kind, q_strides[0], kv_strides[0], self._angles(rope_cs, B),
-                                           self.tables.data_ptr(), self.rows.data_ptr(), scale, out.data_ptr(), out_strides[0], self._stream()))
+        angles, rows, stream = self._angles(rope_cs, B), self.rows, self._stream()
+        if starts is not None:
+            rows = self._live
+            _check(self.lib.d3_pages_live(self.handle, B, self.rows.data_ptr(), self._starts(starts, B), rows.data_ptr(), stream))
+        _check(self.lib.d3_pages_attention(self.handle, layer, B, q.data_ptr(), k_at, v_at, kind, q_strides[0], kv_strides[0], angles,
+                                           self.tables.data_ptr(), rows.data_ptr(), scale, out.data_ptr(), out_strides[0], stream))
         return out
 
     def fill(self, slots, src: int, first: int, n_layers: int) -> None:

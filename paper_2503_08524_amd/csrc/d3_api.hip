@@ -450,7 +450,7 @@ bool whole_context_attention(const d3_ctx* c, const SeqRuns& runs, bool shared) 
 }
 
 // A decode pass whose sequences' rows are in pages instead of the context's cache.
-struct Paged { const d3_pages* pages; const int32_t *tables, *rows; };
+struct Paged { const d3_pages* pages; const int32_t *tables, *rows, *starts; };
 
 // One pass of `ncols` columns through the listed blocks.  hidden_dump (or NULL): dev
 // [(n_ids+1)][dump_cols][d], fed from columns [dump_first, dump_first + dump_cols).
@@ -458,7 +458,7 @@ struct Paged { const d3_pages* pages; const int32_t *tables, *rows; };
 // pos_begin only, and there is no head); picks: its last positions, which hidden_dump takes.
 // fp32_projections: fp32 activations on the vector ALUs also where the pass has several columns.
 // cut_len > 0: the context's splits are so many rows long, instead of as the pass's columns would have them.
-// paged: column c is sequence c's newest row in these pages (cm then says nothing but that every column is a sequence).
+// paged: column c is sequence c's newest row in these pages (cm then says nothing but that every column is a sequence); with starts, a sequence that got no row is idle.
 // save_before >= 0: the residual that enters the first listed block >= save_before (the one after the last, if none)
 // is copied to the workspace's h_skip: it is what the blocks of the drop window would have seen.
 int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_t* ids, int n_ids,
@@ -505,7 +505,9 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
     auto form = [&](int K) { return lines ? split_lines() : split_planes(K, c->lay.split_cols); };
     const EmbedSplit split{mfma ? gain_after(-1) : nullptr, n_split, ssq, form(dm)};
     int2* col_at = qtile ? c->at<int2>(c->lay.col_at) : nullptr;
-    if (paged) D3_HIP(launch_embed_paged(c->tok_emb, d.weight_dtype, tokens, paged->rows, paged->pages->desc.max_pages * paged->pages->desc.page_rows, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, split, s));
+    int32_t* const live = c->at<int32_t>(c->lay.part_ml);      // of a paged pass with starts (the partial results of the context's own attention, which it does not run)
+    const int32_t* const paged_rows = paged && paged->starts ? live : paged ? paged->rows : nullptr;
+    if (paged) D3_HIP(launch_embed_paged(c->tok_emb, d.weight_dtype, tokens, paged->rows, paged->pages->desc.max_pages * paged->pages->desc.page_rows, paged->starts, live, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, split, s));
     else if (qtile) D3_HIP(launch_embed_runs(c->tok_emb, tokens, runs, cm.P, cm.pos_begin, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, row0, col_at, split, s));
     else D3_HIP(launch_embed(c->tok_emb, d.weight_dtype, tokens, cm, ncols, dm, d.vocab, x, c->at<double>(c->lay.inv_freq), hd / 2, rope_cs, row0, split, s));
     auto dump = [&](int slot) -> int {
@@ -581,7 +583,7 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
             PagedAttnArgs pa = paged_attn_args(paged->pages, l, ncols);
             pa.q = qkv; pa.k_new = qkv + qdim; pa.v_new = qkv + qdim + kvdim; pa.dtype = D3_F32;
             pa.q_stride = qkv_dim; pa.kv_stride = qkv_dim; pa.out_stride = qdim;
-            pa.rope_cs = rope_cs; pa.tables = paged->tables; pa.rows = paged->rows;
+            pa.rope_cs = rope_cs; pa.tables = paged->tables; pa.rows = paged_rows;
             pa.out = at.out; pa.out_split = at.out_split; pa.out_form = at.out_form;
             Timed t(c, D3_K_ATTN, s);
             D3_HIP(launch_attention_paged(pa, hd, d.kv_dtype, c->n_cu, s));
@@ -658,7 +660,7 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
             Timed t(c, D3_K_LM_HEAD, s);
             D3_HIP(alu(g, MODE_STORE, true));
         }
-        D3_HIP(launch_argmax(head->logits, d.vocab, head->n_cols, head->tok_out, s));
+        D3_HIP(launch_argmax(head->logits, d.vocab, head->n_cols, head->tok_out, s, paged_rows, tokens));
     }
     return D3_OK;
 }
@@ -943,25 +945,36 @@ int check_pages(const d3_ctx* ctx, const d3_pages* pages, const char* who, bool 
     return D3_OK;
 }
 
+int decode_step_pages(const char* who, d3_ctx* ctx, d3_pages* pages, const int32_t* tok_in, int32_t B, int32_t step_i, const int32_t* tables, const int32_t* rows,
+                      const int32_t* starts, int32_t* tok_out, float* logits, float* hidden_dump, void* hip_stream) {
+    int rc = check_pages(ctx, pages, who, true);
+    if (rc != D3_OK) return rc;
+    if (!ctx->has_plan) return fail(D3_ESTATE, "%s: no plan set (call d3_set_plan)", who);
+    if (step_i < 0 || step_i >= ctx->n_steps) return fail(D3_ERANGE, "%s: step %d is outside the plan of %d steps", who, step_i, ctx->n_steps);
+    const int most = std::min(ctx->desc.max_batch, pages->desc.max_batch);
+    if (B < 1 || B > most) return fail(D3_ESHAPE, "%s: B must be in [1, %d] (got %d)", who, most, B);
+    if (ctx->fill_mode == D3_FILL_RECOMPUTE)                    // that fill reads what the latest step on the context's own cache left in the workspace
+        return fail(D3_ESTATE, "%s: the RECOMPUTE fill is of the context's own cache", who);
+    const OnDevice on(ctx->dev);
+    const Paged paged{pages, tables, rows, starts};
+    const ColMap cm{0, B, 1, 0};
+    const HeadOut head{0, B, logits ? logits : ctx->at<float>(ctx->lay.logits), tok_out};
+    return forward(ctx, tok_in, cm, B, ctx->layer_ids.data() + (size_t)step_i * ctx->desc.n_layers, ctx->keep[step_i], hidden_dump, 0, B, &head,
+                   static_cast<hipStream_t>(hip_stream), -1, -1, 0, nullptr, nullptr, false, 0, &paged);
+}
+
 }  // namespace
 
 extern "C" int d3_decode_step_paged(d3_ctx* ctx, d3_pages* pages, const int32_t* tok_in, int32_t B, int32_t step_i, const int32_t* tables,
                                     const int32_t* rows, int32_t* tok_out, float* logits, float* hidden_dump, void* hip_stream) {
     if (!ctx || !pages || !tok_in || !tables || !rows || !tok_out) return fail(D3_EINVAL, "d3_decode_step_paged: NULL argument");
-    int rc = check_pages(ctx, pages, "d3_decode_step_paged", true);
-    if (rc != D3_OK) return rc;
-    if (!ctx->has_plan) return fail(D3_ESTATE, "d3_decode_step_paged: no plan set (call d3_set_plan)");
-    if (step_i < 0 || step_i >= ctx->n_steps) return fail(D3_ERANGE, "d3_decode_step_paged: step %d is outside the plan of %d steps", step_i, ctx->n_steps);
-    const int most = std::min(ctx->desc.max_batch, pages->desc.max_batch);
-    if (B < 1 || B > most) return fail(D3_ESHAPE, "d3_decode_step_paged: B must be in [1, %d] (got %d)", most, B);
-    if (ctx->fill_mode == D3_FILL_RECOMPUTE)                    // that fill reads what the latest step on the context's own cache left in the workspace
-        return fail(D3_ESTATE, "d3_decode_step_paged: the RECOMPUTE fill is of the context's own cache");
-    const OnDevice on(ctx->dev);
-    const Paged paged{pages, tables, rows};
-    const ColMap cm{0, B, 1, 0};
-    const HeadOut head{0, B, logits ? logits : ctx->at<float>(ctx->lay.logits), tok_out};
-    return forward(ctx, tok_in, cm, B, ctx->layer_ids.data() + (size_t)step_i * ctx->desc.n_layers, ctx->keep[step_i], hidden_dump, 0, B, &head,
-                   static_cast<hipStream_t>(hip_stream), -1, -1, 0, nullptr, nullptr, false, 0, &paged);
+    return decode_step_pages("d3_decode_step_paged", ctx, pages, tok_in, B, step_i, tables, rows, nullptr, tok_out, logits, hidden_dump, hip_stream);
+}
+
+extern "C" int d3_decode_step_granted(d3_ctx* ctx, d3_pages* pages, const int32_t* tok_in, int32_t B, int32_t step_i, const int32_t* tables, const int32_t* rows,
+                                      const int32_t* starts, int32_t* tok_out, float* logits, float* hidden_dump, void* hip_stream) {
+    if (!ctx || !pages || !tok_in || !tables || !rows || !starts || !tok_out) return fail(D3_EINVAL, "d3_decode_step_granted: NULL argument");
+    return decode_step_pages("d3_decode_step_granted", ctx, pages, tok_in, B, step_i, tables, rows, starts, tok_out, logits, hidden_dump, hip_stream);
 }
 
 extern "C" int d3_store_pages(d3_ctx* ctx, d3_pages* pages, int32_t seq, int32_t row_begin, int32_t n, const int32_t* slots, void* hip_stream) {

@@ -317,8 +317,8 @@ int launch_pick_rows(const float* x, int d, const RowPick& pick, float* dst, hip
 int launch_embed(const void* tok_emb, int weight_dtype, const int32_t* tokens, ColMap cm, int ncols, int d,
                  int vocab, float* x, const double* inv_freq, int half_hd, float2* rope_cs, const int* row0, const EmbedSplit& split, hipStream_t s);
 
-// A decode step on pages: sequence c's token is its row min(rows[c], max_rows) - 1.
-int launch_embed_paged(const void* tok_emb, int weight_dtype, const int32_t* tokens, const int32_t* rows, int max_rows, int ncols, int d, int vocab,
+// A decode step on pages: sequence c's token is its row min(rows[c], max_rows) - 1.  With starts (optional, [ncols + 1], of a reserve), live[c] becomes the rows of the sequences that got some, 0 for the others.
+int launch_embed_paged(const void* tok_emb, int weight_dtype, const int32_t* tokens, const int32_t* rows, int max_rows, const int32_t* starts, int32_t* live, int ncols, int d, int vocab,
                        float* x, const double* inv_freq, int half_hd, float2* rope_cs, const EmbedSplit& split, hipStream_t s);
 
 struct RopeArgs {
@@ -356,7 +356,8 @@ int launch_attention(const AttnArgs& a, int kv_dtype, bool use_mfma, hipStream_t
 
 int launch_attention_prompt(const AttnArgs& a, const SeqRuns& runs, int kv_dtype, hipStream_t s);   // attention_prompt.hip
 
-int launch_argmax(const float* logits, int vocab, int ncols, int32_t* out, hipStream_t s);
+// rows (optional): a column whose sequence has none keeps its token, tok_in[c]; tok_in may be out.
+int launch_argmax(const float* logits, int vocab, int ncols, int32_t* out, hipStream_t s, const int32_t* rows = nullptr, const int32_t* tok_in = nullptr);
 
 struct FillArgs {
     void* k_cache;         // whole cache [L][max_batch][H_kv][max_seq][hd]

@@ -150,6 +150,14 @@ extern "C" int d3_pages_reserve(d3_pages* pages, int32_t B, const int32_t* added
     return D3_OK;
 }
 
+extern "C" int d3_pages_live(d3_pages* pages, int32_t B, const int32_t* rows, const int32_t* starts, int32_t* live, void* hip_stream) {
+    if (!pages || !rows || !starts || !live) return fail(D3_EINVAL, "d3_pages_live: NULL argument");
+    D3_CHECK(check_batch(pages, "d3_pages_live", B));
+    const OnDevice on(pages->dev);
+    D3_HIP(launch_pages_live(rows, starts, pages->desc.max_pages * pages->desc.page_rows, B, live, static_cast<hipStream_t>(hip_stream)));
+    return D3_OK;
+}
+
 extern "C" int d3_pages_append(d3_pages* pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t* slots, const void* k, const void* v, int32_t dtype,
                                int64_t token_stride, int64_t head_stride, int64_t layer_stride, const float* rope_cs, void* hip_stream) {
     if (!pages) return fail(D3_EINVAL, "d3_pages_append: pages is NULL");

@@ -1,6 +1,7 @@
 // Small kernels around the projections: embedding gather, gain + bf16 split for
 // the MFMA path, rotary embedding + KV append, greedy argmax, missing-state KV fill.
 #include "d3_common.h"
+#include "pages.h"
 
 namespace d3 {
 
@@ -88,10 +89,11 @@ __global__ __launch_bounds__(256) void embed_runs_kernel(const bf16_t* __restric
 }
 template <typename W>
 __global__ __launch_bounds__(256) void embed_paged_kernel(const W* __restrict__ emb, const int32_t* __restrict__ tokens, const int32_t* __restrict__ rows,
-                                                          int max_rows, int d, int vocab, float* __restrict__ x, const double* __restrict__ inv_freq, int half_hd,
-                                                          float2* __restrict__ rope_cs, EmbedSplit split) {
-    const int c = blockIdx.x;
-    embed_column<W>(emb, tokens[c], max(min(rows[c], max_rows) - 1, 0), c, d, vocab, x, inv_freq, half_hd, rope_cs, split);
+                                                          int max_rows, const int32_t* __restrict__ starts, int32_t* __restrict__ live, int d, int vocab, float* __restrict__ x,
+                                                          const double* __restrict__ inv_freq, int half_hd, float2* __restrict__ rope_cs, EmbedSplit split) {
+    const int c = blockIdx.x, n = live_rows(rows, starts, max_rows, c);
+    if (starts && threadIdx.x == 0) live[c] = n;
+    embed_column<W>(emb, tokens[c], max(n - 1, 0), c, d, vocab, x, inv_freq, half_hd, rope_cs, split);
 }
 
 // ---------------- the last positions of a prompt pass ----------------
@@ -205,12 +207,13 @@ __device__ __forceinline__ Best best_of_wave(Best b) {
     i = __builtin_amdgcn_permlane16_swap((unsigned)b.i, (unsigned)b.i, false, false);
     return best_of_row(better(Best{__uint_as_float(v[0]), (int)i[0]}, Best{__uint_as_float(v[1]), (int)i[1]}));
 }
-__global__ __launch_bounds__(1024) void argmax_kernel(const float* __restrict__ logits, int vocab, int32_t* __restrict__ out) {
+__global__ __launch_bounds__(1024) void argmax_kernel(const float* __restrict__ logits, int vocab, int32_t* out, const int32_t* rows, const int32_t* tok_in) {
     constexpr int R = 16;                              // pairs of logits in flight per thread
     __shared__ float bv[16];
     __shared__ int bi[16];
     const int c = blockIdx.x, tid = threadIdx.x;
     const float* lg = logits + (size_t)c * vocab;
+    const bool keeps = rows && rows[c] <= 0;
     Best best{-INFINITY, 0x7fffffff};
     const int n2 = vocab / 2;                          // vocab % 2 == 0
     for (int base = 0; base < n2; base += 1024 * R) {
@@ -233,7 +236,7 @@ __global__ __launch_bounds__(1024) void argmax_kernel(const float* __restrict__ 
     __syncthreads();
     if (tid < 16) {
         best = best_of_row(Best{bv[tid], bi[tid]});
-        if (tid == 0) out[c] = best.i >= vocab ? 0 : best.i;
+        if (tid == 0) out[c] = keeps ? tok_in[c] : best.i >= vocab ? 0 : best.i;
     }
 }
 
@@ -318,13 +321,13 @@ int launch_embed(const void* tok_emb, int weight_dtype, const int32_t* tokens, C
     return (int)hipGetLastError();
 }
 
-int launch_embed_paged(const void* tok_emb, int weight_dtype, const int32_t* tokens, const int32_t* rows, int max_rows, int ncols, int d, int vocab,
+int launch_embed_paged(const void* tok_emb, int weight_dtype, const int32_t* tokens, const int32_t* rows, int max_rows, const int32_t* starts, int32_t* live, int ncols, int d, int vocab,
                        float* x, const double* inv_freq, int half_hd, float2* rope_cs, const EmbedSplit& split, hipStream_t s) {
     if (weight_dtype == 0)
-        hipLaunchKernelGGL(embed_paged_kernel<float>, dim3(ncols), dim3(256), 0, s, static_cast<const float*>(tok_emb), tokens, rows, max_rows, d, vocab, x,
+        hipLaunchKernelGGL(embed_paged_kernel<float>, dim3(ncols), dim3(256), 0, s, static_cast<const float*>(tok_emb), tokens, rows, max_rows, starts, live, d, vocab, x,
                            inv_freq, half_hd, rope_cs, split);
     else
-        hipLaunchKernelGGL(embed_paged_kernel<bf16_t>, dim3(ncols), dim3(256), 0, s, static_cast<const bf16_t*>(tok_emb), tokens, rows, max_rows, d, vocab, x,
+        hipLaunchKernelGGL(embed_paged_kernel<bf16_t>, dim3(ncols), dim3(256), 0, s, static_cast<const bf16_t*>(tok_emb), tokens, rows, max_rows, starts, live, d, vocab, x,
                            inv_freq, half_hd, rope_cs, split);
     return (int)hipGetLastError();
 }
@@ -355,8 +358,8 @@ int launch_rope_append(const RopeArgs& a, int kv_dtype, hipStream_t s) {
     return (int)hipGetLastError();
 }
 
-int launch_argmax(const float* logits, int vocab, int ncols, int32_t* out, hipStream_t s) {
-    hipLaunchKernelGGL(argmax_kernel, dim3(ncols), dim3(1024), 0, s, logits, vocab, out);
+int launch_argmax(const float* logits, int vocab, int ncols, int32_t* out, hipStream_t s, const int32_t* rows, const int32_t* tok_in) {
+    hipLaunchKernelGGL(argmax_kernel, dim3(ncols), dim3(1024), 0, s, logits, vocab, out, rows, tok_in);
     return (int)hipGetLastError();
 }
 

@@ -27,6 +27,12 @@ struct ReserveArgs {
     int32_t *rows_out, *n_free_out, *tables, *free_pages, *starts, *slots, *positions;
 };
 int launch_pages_reserve(const ReserveArgs& a, hipStream_t s);
+// Rows of a sequence as a step counts them: none where a reserve with these starts (optional) gave it none.
+__device__ __forceinline__ int live_rows(const int32_t* rows, const int32_t* starts, int max_rows, int b) {
+    const int n = min(max(rows[b], 0), max_rows);
+    return starts && starts[b] == starts[b + 1] ? 0 : n;
+}
+int launch_pages_live(const int32_t* rows, const int32_t* starts, int max_rows, int B, int32_t* live, hipStream_t s);
 
 struct AppendArgs {
     int n, n_layers, H_kv, hd, page_shift;

@@ -175,6 +175,11 @@ __global__ __launch_bounds__(256) void pages_slots_kernel(ReserveArgs a) {
     if (t < a.max_tokens) write_token(a, starts, t);
 }
 
+__global__ __launch_bounds__(256) void pages_live_kernel(const int32_t* rows, const int32_t* starts, int max_rows, int B, int32_t* live) {
+    const int b = blockIdx.x * 256 + threadIdx.x;
+    if (b < B) live[b] = live_rows(rows, starts, max_rows, b);
+}
+
 // ---------------- rows into pages ----------------
 // E adjacent elements, 16 bytes of S or T at a time
 template <int E, typename S> __device__ __forceinline__ void load_many(const S* p, float (&y)[E]) {
@@ -374,6 +379,11 @@ int launch_pages_reserve(const ReserveArgs& a, hipStream_t s) {
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || few) return (int)e;
     hipLaunchKernelGGL(pages_slots_kernel, dim3((a.max_tokens + 255) / 256), dim3(256), 0, s, a);
+    return (int)hipGetLastError();
+}
+
+int launch_pages_live(const int32_t* rows, const int32_t* starts, int max_rows, int B, int32_t* live, hipStream_t s) {
+    hipLaunchKernelGGL(pages_live_kernel, dim3((B + 255) / 256), dim3(256), 0, s, rows, starts, max_rows, B, live);
     return (int)hipGetLastError();
 }
 

@@ -84,3 +84,9 @@ def test_attention_keeps_its_rows_in_registers(tmp_path):
     for field, most in ((".private_segment_fixed_size", 0), (".vgpr_spill_count", 0), (".vgpr_count", 256)):
         found = [int(x) for x in re.findall(re.escape(field) + r":\s+(\d+)", text)]
         assert len(found) == 16 and max(found) <= most, (field, found)
+
+
+def test_null_handles_are_errors_of_the_calls_with_starts(lib):
+    for call, args in ((lib.d3_pages_live, (None, 1, None, None, None, None)),
+                       (lib.d3_decode_step_granted, (None, None, None, 1, 1, None, None, None, None, None, None, None))):
+        assert call(*args) == -1 and "NULL" in lib.d3_last_error().decode()
