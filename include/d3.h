@@ -258,7 +258,7 @@ size_t d3_pages_workspace_size(const d3_pages_desc *desc);
 int d3_pages_create(d3_pages **out, const d3_pages_desc *desc, void *k_pages, void *v_pages, void *workspace, size_t workspace_bytes);
 int d3_pages_destroy(d3_pages *pages);
 
-/* Page tables and slot maps from request lengths.  added: dev int32 [B]: how many rows sequence b asks for (0: none; negative: the sequence has
+/* Page tables and slot maps from request lengths.  Granted pages are not cleared: they hold what their last owner left.  added: dev int32 [B]: how many rows sequence b asks for (0: none; negative: the sequence has
  * ended, its pages go back and its rows become 0).  Pages of ended sequences are pushed first, in the order of b and of their tables.  Then the
  * requests are granted in the order of b, whole or not at all: b is refused if its rows would pass max_pages * page_rows; else if the rows asked for
  * up to and including it pass max_tokens; else if it needs pages and those needed up to and including it (by requests not refused so far for the other
@@ -302,8 +302,11 @@ int d3_store_pages(d3_ctx *ctx, d3_pages *pages, int32_t seq, int32_t row_begin,
 
 /* One decode step (as d3_decode_step) of B sequences whose rows are in `pages`: sequence b's token is row rows[b] - 1, for which d3_pages_reserve has made
  * room, and its rotary position; a sequence without rows is idle (tok_out[b] = tok_in[b], its logits and hidden_dump mean nothing).  Only for callers who know that every sequence with rows has got
- * one: of a sequence that was refused or asked for none the step would overwrite the newest row (d3_decode_step_granted leaves it as it is).  Runs the blocks of step `step_i` of the plan, 0 <= step_i < n_steps, in any order
- * of steps; the context's own cache, row count and step counter stay as they are.  D3_ESHAPE unless the pages have the context's shape and cache type;
+ * one: of a sequence that was refused or asked for none the step would overwrite the newest row (d3_decode_step_granted leaves it as it is).  Runs the blocks of step `step_i` of the
+ * plan, 0 <= step_i < n_steps, in any order of steps; the context's own cache, row count and step counter stay as they are.  A block that the step drops gets no row: until
+ * d3_fill_missing_paged has filled it, the pages hold there what they held before, another request's row if they are another's former pages.  So a step is followed by the fill of its
+ * slots before any step that runs a block it dropped; only where every later step of these sequences drops these blocks too (a request's own steps in order, by a shrinking depth) it may be left out.
+ * D3_ESHAPE unless the pages have the context's shape and cache type;
  * D3_ESTATE with D3_FILL_RECOMPUTE. */
 int d3_decode_step_paged(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, int32_t B, int32_t step_i, const int32_t *tables,
                          const int32_t *rows, int32_t *tok_out, float *logits, float *hidden_dump, void *hip_stream);
@@ -314,7 +317,8 @@ int d3_decode_step_paged(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, in
 int d3_decode_step_granted(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, int32_t B, int32_t step_i, const int32_t *tables, const int32_t *rows,
                            const int32_t *starts, int32_t *tok_out, float *logits, float *hidden_dump, void *hip_stream);
 
-/* d3_pages_fill of the blocks that step `step_i` of the context's plan drops, from the block d3_fill_missing_kv takes (Section 3.2). */
+/* d3_pages_fill of the blocks that step `step_i` of the context's plan drops, from the block d3_fill_missing_kv takes (Section 3.2): of the rows `slots` that the reserve before a step
+ * gave (entries of -1 are skipped), after that step. */
 int d3_fill_missing_paged(d3_ctx *ctx, d3_pages *pages, int32_t step_i, int32_t n, const int32_t *slots, void *hip_stream);
 
 /* Measurement aid: per-launch timing of one kernel class with HIP events recorded

@@ -263,7 +263,7 @@ class Decoder:
     def decode_step_paged(self, cache: "PagedCache", tok_in, step_i: int, tok_out, logits=None, hidden_dump=None, starts=None) -> None:
         """One step of the cache's first tok_in.numel() sequences, whose newest rows cache.reserve has made room for.  starts: what that reserve returned; the sequences
         that it gave no row (refused, paused, ended) are idle: their rows stay, tok_out is tok_in.  Without it every sequence that has rows must have got one, or
-        the step overwrites its newest row."""
+        the step overwrites its newest row.  fill_missing_paged of that reserve's slots comes next, before any step that runs a block this one drops."""
         cache._ints(tok_in=tok_in, tok_out=tok_out)
         B = tok_in.numel()
         if tok_out.numel() < B:
@@ -276,7 +276,7 @@ class Decoder:
             _check(self.lib.d3_decode_step_granted(*at, cache._starts(starts, B), *out))
 
     def fill_missing_paged(self, cache: "PagedCache", slots, step_i: int) -> None:
-        """COPY fill of the rows `slots` in the blocks that step step_i of the plan drops."""
+        """COPY fill of the rows `slots`, which a reserve returned, in the blocks that step step_i of the plan drops, after that step: the pages hold there what their last owner left."""
         cache._ints(slots=slots)
         _check(self.lib.d3_fill_missing_paged(self.ctx, cache.handle, step_i, slots.numel(), slots.data_ptr(), self._stream()))
 

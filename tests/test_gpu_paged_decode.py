@@ -219,3 +219,39 @@ def test_refusals():
         dec.decode_step_paged(cache, tok, 1, tok[:1])
     with pytest.raises(ValueError):
         dec.store_pages(cache, 0, tok.long())
+
+
+@pytest.mark.parametrize("order", [[5, 4, 3, 2, 1, 0], [3, 5, 0, 4, 1, 2]])
+@pytest.mark.parametrize("kv", ["f16", "f32"])
+def test_steps_in_any_order_on_pages_that_held_other_rows(order, kv):
+    """Each step followed by the fill of its rows: a block that an earlier step dropped finds the rows it attends over.  Pools of NaN (what another request left may be anything) against
+    the context's own cache with a plan of the same depths in that order."""
+    import math
+    import torch
+    from paper_2503_08524_amd import binding
+    B, P, lengths = 3, 21, [21, 16, 6]
+    w = d3_inputs.make_weights(GQA, 0)
+    dec = _decoder(GQA, w, B, P + 8, kv)
+    keep, drop, _ = binding.d3_plan_depth(GQA.L, 0.75, 1, 0, 6)
+    assert len(set(keep.tolist())) >= 3
+    prompts = torch.from_numpy(d3_inputs.make_prompt(B, P, GQA.V, seed=31)).to(DEV)
+    forced = torch.from_numpy(d3_inputs.make_prompt(6, B, GQA.V, seed=32)).to(DEV)
+    dec.set_plan_table(np.concatenate([[GQA.L], keep[order]]), np.concatenate([[0], drop[order]]))
+    logits, nxt, want = torch.zeros(B, GQA.V, device=DEV), torch.zeros(B, dtype=torch.int32, device=DEV), []
+    dec.prefill_ragged(prompts, lengths)
+    for n in range(6):
+        dec.decode_step(forced[n], n + 1, nxt, logits=logits)
+        dec.fill_missing_kv(dec.n_ctx - 1, dec.n_ctx)
+        want.append(logits.clone())
+    dec.set_plan(0.75, 1, 0, 6)
+    dec.prefill_ragged(prompts, lengths)
+    cache = _pages(dec, 9, B, P + 8)
+    cache.k_pages.fill_(math.nan)
+    cache.v_pages.fill_(math.nan)
+    _admit(dec, cache, lengths)
+    for n, step in enumerate(order):
+        starts, slots, _ = cache.reserve(torch.ones(B, dtype=torch.int32, device=DEV), B)
+        dec.decode_step_paged(cache, forced[n], step, nxt, logits=logits, starts=starts)
+        dec.fill_missing_paged(cache, slots, step)
+        # fp32 rows differ by the order of sums; an fp16 row that is rounded the other way for that is 2^-11 of itself off
+        assert (logits - want[n]).abs().max() < (1e-4 if kv == "f32" else helpers.LOGIT_ATOL), (n, step)
