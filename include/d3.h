@@ -254,7 +254,8 @@ typedef struct d3_pages d3_pages;
 size_t d3_pages_workspace_size(const d3_pages_desc *desc);
 
 /* Handle on caller-owned pools and workspace (256-byte aligned, d3_pages_workspace_size bytes; pools 16-byte aligned), on the current
- * device, which the calls below make current for themselves.  Clears the counters on the null stream and waits for it. */
+ * device, which the calls below make current for themselves.  Clears the counters on the null stream and waits for it: no work on another stream may be using the workspace's
+ * memory, and no stream may be capturing. */
 int d3_pages_create(d3_pages **out, const d3_pages_desc *desc, void *k_pages, void *v_pages, void *workspace, size_t workspace_bytes);
 int d3_pages_destroy(d3_pages *pages);
 

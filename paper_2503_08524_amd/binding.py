@@ -312,7 +312,8 @@ class Decoder:
 class PagedCache:
     """A paged key-value cache (the d3_pages_* entry points) and the operators on it: one handle, the page pools and the
     state of the sequences, all torch tensors on one GPU.  Every call is asynchronous on the current stream, allocates nothing on the
-    device unless an output is left out, and can be captured into a graph.
+    device unless an output is left out, and can be captured into a graph.  Making one waits for the current stream and cannot be captured; before one that other
+    streams have used goes away, these have to be waited for.
 
     k_pages [n_layers][n_pages][n_kv_heads][page_rows][head_dim] and v_pages [n_layers][n_pages][n_kv_heads][page_rows / R][head_dim][R]
     (R = 8 for "f16", 4 for "f32"); tables int32 [max_batch][max_pages]; rows int32 [max_batch]; free_pages int32 [n_pages], a stack of which
@@ -362,6 +363,8 @@ class PagedCache:
                 self.n_free[:1].fill_(n_pages)
             self._live = torch.empty(max_batch, dtype=torch.int32, device=self.device)      # rows that an attend with starts counts
             self.workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+            # The counters are cleared on the null stream, which does not wait for this one, where work on memory that the workspace was made from may still be queued.
+            torch.cuda.current_stream(self.device).synchronize()
             handle = C.c_void_p()
             _check(self.lib.d3_pages_create(C.byref(handle), C.byref(desc), self.k_pages.data_ptr(), self.v_pages.data_ptr(),
                                             self.workspace.data_ptr(), ws_bytes))
