@@ -114,8 +114,9 @@ size_t d3_workspace_size(const d3_model_desc *desc);
 
 /* Build a context around caller-owned device buffers.  k_cache / v_cache: dev,
  * [L][max_batch][H_kv][max_seq][head_dim] of kv_dtype.  workspace: dev,
- * d3_workspace_size() bytes, 256-byte aligned; the library keeps the residual
- * stream, activations, attention partials and the layer-index table there.  With
+ * d3_workspace_size() bytes, 256-byte aligned, used by no work on any stream when
+ * the call is made; the library keeps the residual stream, activations, attention
+ * partials and the layer-index table there.  With
  * fewer bytes prompt passes are narrower (prompts take longer); D3_EINVAL, with the
  * fewest that will do in the message, only below those.
  * D3_ESHAPE unless head_dim in {64,128}, n_heads % n_kv_heads == 0,

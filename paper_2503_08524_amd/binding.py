@@ -195,6 +195,8 @@ class Decoder:
                     setattr(layers[l], name, t.data_ptr())
             self._layers = layers
             w = _Weights(weights["tok_emb"].data_ptr(), layers, weights["final_norm"].data_ptr(), weights["lm_head"].data_ptr())
+            # d3_create writes to the workspace on the null stream, which does not wait for this one, where the zeros are still to be written.
+            torch.cuda.current_stream(self.device).synchronize()
             ctx = C.c_void_p()
             _check(self.lib.d3_create(C.byref(ctx), C.byref(desc), C.byref(w), self.k_cache.data_ptr(), self.v_cache.data_ptr(),
                                       self.workspace.data_ptr(), ws_bytes))

@@ -41,3 +41,29 @@ def test_a_paged_cache_whose_workspace_is_still_written():
             torch.cuda.current_stream().synchronize()
             assert all(torch.equal(x, want) for x in out)
     assert reused
+
+
+def test_a_decoder_whose_workspace_is_still_written():
+    """Frequencies and counters lie in the workspace: a decoder made on a busy side stream gives the logits of one made in quiet."""
+    import torch
+    from paper_2503_08524_amd import binding
+    w = binding.weights_to_device(steps.GQA, d3_inputs.make_weights(steps.GQA, 0), DEV)
+    tok = torch.from_numpy(d3_inputs.make_prompt(2, 20, steps.GQA.V, seed=7)).to(DEV)
+
+    def run():
+        dec = binding.Decoder(steps.GQA, w, 2, 32, kv_dtype="f16", device=DEV)
+        dec.set_plan(1.0, 0, 0, 3)
+        logits = [torch.zeros(2, steps.GQA.V, device=DEV) for _ in range(3)]
+        nxt = dec.prefill(tok, logits=logits[0])
+        for i in (1, 2):
+            dec.decode_step(nxt, i, nxt, logits=logits[i])
+        torch.cuda.current_stream().synchronize()
+        return dec, logits
+    dec, want = run()
+    size = dec.workspace.numel()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        for _ in range(3):
+            _busy_block(size)
+            got = run()[1]
+            assert all(torch.equal(x, y) for x, y in zip(got, want)) and all(np.isfinite(x.cpu().numpy()).all() for x in got)
