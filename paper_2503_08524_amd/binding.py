@@ -402,9 +402,10 @@ class PagedCache:
         return rope_cs.data_ptr()
 
     def _heads(self, name: str, t, dims, dtype, strides=None):
-        """The tensor's strides; it must have these dims, this dtype, a dense last dim (and these strides)."""
+        """The tensor's strides; it must have these dims, this dtype, a dense last dim (and these strides, where a dim has more than one entry)."""
         own = t.stride()
-        if t.shape != dims or t.dtype is not dtype or t.get_device() != self._index or own[-1] != 1 or (strides is not None and own != strides):
+        if (t.shape != dims or t.dtype is not dtype or t.get_device() != self._index or own[-1] != 1
+                or (strides is not None and own != strides and any(x != y and n > 1 for x, y, n in zip(own, strides, dims)))):
             raise ValueError(f"{name} must be a {dtype} tensor {tuple(dims)} on {self.device}, its last dim dense{'' if strides is None else f', with strides {strides}'}")
         return own
 
@@ -436,7 +437,8 @@ class PagedCache:
         return starts, slots, positions
 
     def append(self, layer: int, slots, k, v, rope_cs=None) -> None:
-        """k, v [n][n_kv_heads][head_dim], or [m][n][n_kv_heads][head_dim] for the m layers from `layer` on, into the rows `slots` (int32 CUDA tensor [n]) of the pools.
+        """k, v [n][n_kv_heads][head_dim], or [m][n][n_kv_heads][head_dim] for the m layers from `layer` on, into the rows `slots` (int32 CUDA tensor [n]) of the pools.  k and v have
+        the same strides, the last dim dense.
         rope_cs [n][head_dim / 2][2]: (cos, sin) by which the keys turn first."""
         self._ints(slots=slots)
         n, kind = slots.numel(), self._kind(k)
@@ -444,12 +446,14 @@ class PagedCache:
         dims = (layers, n, self.n_kv_heads, self.head_dim) if k.dim() == 4 else (n, self.n_kv_heads, self.head_dim)
         strides = self._heads("k", k, dims, k.dtype)
         self._heads("v", v, dims, k.dtype, strides)
-        _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, strides[-3], strides[-2],
-                                        strides[0] if len(strides) == 4 else 0, self._angles(rope_cs, n), self._stream()))
+        # (the stride of a dim with one entry says nothing)
+        _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, strides[-3] if n > 1 else 0,
+                                        strides[-2] if self.n_kv_heads > 1 else 0, strides[0] if layers > 1 else 0, self._angles(rope_cs, n), self._stream()))
 
     def attend(self, layer: int, q, k=None, v=None, rope_cs=None, scale: float = 0.0, out=None, starts=None):
         """Attention of one token of each of the first B sequences, q [B][n_heads][head_dim], over their rows; returns out [B][n_heads][head_dim] of q's dtype.
-        k, v [B][n_kv_heads][head_dim]: the newest rows (row rows[b] - 1), which the call also writes to their pages; without them they are there already.
+        k, v [B][n_kv_heads][head_dim]: the newest rows (row rows[b] - 1), which the call also writes to their pages; without them they are there already.  The heads of a
+        sequence lie side by side in all of them, and k and v have the same strides.
         rope_cs [B][head_dim / 2][2]: q and k turn by it.  scale 0: 1 / sqrt(head_dim).
         starts: what the reserve before it returned; of the sequences that it gave no row nothing is read or written, and out is 0.  Without it, and with k and v, every sequence
         that has rows must have got one."""
@@ -458,7 +462,7 @@ class PagedCache:
         if out is None:
             out = self.torch.empty(dims, dtype=dtype, device=self.device)
         q_strides, out_strides = self._heads("q", q, dims, dtype), self._heads("out", out, dims, dtype)
-        if q_strides[1] != self.head_dim or out_strides[1] != self.head_dim:
+        if self.n_heads > 1 and (q_strides[1] != self.head_dim or out_strides[1] != self.head_dim):
             raise ValueError("q and out must have the heads of a sequence side by side")
         k_at = v_at = None
         kv_strides = (0,)
@@ -466,11 +470,13 @@ class PagedCache:
             dims = (B, self.n_kv_heads, self.head_dim)
             kv_strides = self._heads("k", k, dims, dtype)
             self._heads("v", v, dims, dtype, kv_strides)
-            if kv_strides[1] != self.head_dim:
+            if self.n_kv_heads > 1 and kv_strides[1] != self.head_dim:
                 raise ValueError("k and v must have the heads of a sequence side by side")
             k_at, v_at = k.data_ptr(), v.data_ptr()
         elif k is not None or v is not None:
             raise ValueError("k and v come together or not at all")
+        if B == 1:                                                  # (the stride of a dim with one entry says nothing)
+            q_strides = kv_strides = out_strides = (0,)
         angles, rows, stream = self._angles(rope_cs, B), self.rows, self._stream()
         if starts is not None:
             rows = self._live

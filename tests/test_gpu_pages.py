@@ -737,3 +737,45 @@ def test_more_rows_than_a_launch_counts_are_refused():
         assert word in cache.lib.d3_last_error().decode()
     assert cache.lib.d3_pages_fill(cache.handle, (1 << 30) + 1, None, 0, 1, 1, None) == -1
     torch.cuda.synchronize()
+
+
+def test_strides_of_dims_with_one_entry_say_nothing():
+    """One sequence, one token, one layer, one head: whatever torch calls the stride of such a dim, the call is that of the dense tensor."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+
+    def odd(x, at):
+        """The same values, the stride of dim `at` (of one entry) 13."""
+        strides = list(x.stride())
+        strides[at] = 13
+        return x.as_strided(x.shape, strides)
+    for B, heads, group in ((1, 2, 2), (3, 1, 1), (1, 1, 1)):
+        cache, g = _cache([40, 16, 7][:B], heads, group, 64, "f16", 16, seed=15, room=1)
+        q = torch.empty(B, heads * group, 64, device=DEV).normal_(generator=g)
+        k, v = (torch.empty(B, heads, 64, device=DEV).normal_(generator=g) for _ in range(2))
+        want = cache.attend(0, q, k, v)
+        dims = [x for x, n in enumerate((B, heads * group)) if n == 1]
+        for at in dims:
+            out = odd(torch.empty_like(q), at)
+            cache.attend(0, odd(q, at), odd(k, at), v, out=out)
+            assert torch.equal(out, want)
+            cache.attend(0, q, k, odd(v, at), out=out)
+            assert torch.equal(out, want)
+    for layers, n, heads in ((1, 5, 2), (2, 1, 2), (2, 5, 1), (1, 1, 1)):
+        caches = [PagedCache(heads, heads, 64, 4, 16, 1, 1, n_layers=2, device=DEV) for _ in range(2)]
+        k, v = (torch.randn(layers, n, heads, 64, device=DEV) for _ in range(2))
+        slots = torch.arange(3, 3 + n, dtype=torch.int32, device=DEV)
+        caches[0].append(0, slots, k, v)
+        for at in [x for x, m in enumerate((layers, n, heads)) if m == 1]:
+            for kk, vv in ((odd(k, at), v), (k, odd(v, at)), (odd(k, at), odd(v, at))):
+                caches[1].k_pages.zero_()
+                caches[1].v_pages.zero_()
+                caches[1].append(0, slots, kk, vv)
+                assert torch.equal(caches[0].k_pages, caches[1].k_pages) and torch.equal(caches[0].v_pages, caches[1].v_pages)
+    # a dim with more entries is looked at as before
+    cache = PagedCache(2, 2, 64, 4, 16, 2, 1, device=DEV)
+    k = torch.randn(2, 2, 64, device=DEV)
+    for call in (lambda: cache.append(0, torch.zeros(2, dtype=torch.int32, device=DEV), k, k.transpose(0, 1).contiguous().transpose(0, 1)),
+                 lambda: cache.attend(0, k.transpose(0, 1).contiguous().transpose(0, 1))):
+        with pytest.raises(ValueError):
+            call()
