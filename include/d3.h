@@ -320,7 +320,7 @@ int d3_decode_step_granted(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, 
                            const int32_t *starts, int32_t *tok_out, float *logits, float *hidden_dump, void *hip_stream);
 
 /* d3_pages_fill of the blocks that step `step_i` of the context's plan drops, from the block d3_fill_missing_kv takes (Section 3.2): of the rows `slots` that the reserve before a step
- * gave (entries of -1 are skipped), after that step. */
+ * gave (entries of -1 are skipped), after that step.  D3_ESHAPE unless the pages have the context's layers, KV heads and head_dim. */
 int d3_fill_missing_paged(d3_ctx *ctx, d3_pages *pages, int32_t step_i, int32_t n, const int32_t *slots, void *hip_stream);
 
 /* Measurement aid: per-launch timing of one kernel class with HIP events recorded

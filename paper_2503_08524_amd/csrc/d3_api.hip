@@ -936,12 +936,12 @@ extern "C" int d3_decode_step_static(d3_ctx* ctx, const int32_t* tok_in, int32_t
 
 namespace {
 
-// The pages are of the context's shape and on its GPU.
-int check_pages(const d3_ctx* ctx, const d3_pages* pages, const char* who, bool same_type) {
+// The pages' rows are of the context's shape and on its GPU; for a step, its query heads and its cache's type too.
+int check_pages(const d3_ctx* ctx, const d3_pages* pages, const char* who, bool step) {
     const d3_model_desc& d = ctx->desc;
     const d3_pages_desc& p = pages->desc;
-    if (p.n_layers != d.n_layers || p.n_heads != d.n_heads || p.n_kv_heads != d.n_kv_heads || p.head_dim != d.head_dim || (same_type && p.kv_dtype != d.kv_dtype))
-        return fail(D3_ESHAPE, "%s: the pages' layers, heads, head_dim%s must be the context's", who, same_type ? " and type" : "");
+    if (p.n_layers != d.n_layers || p.n_kv_heads != d.n_kv_heads || p.head_dim != d.head_dim || (step && (p.n_heads != d.n_heads || p.kv_dtype != d.kv_dtype)))
+        return fail(D3_ESHAPE, "%s: the pages' layers, %s, head_dim%s must be the context's", who, step ? "heads" : "KV heads", step ? " and type" : "");
     if (pages->dev != ctx->dev) return fail(D3_EINVAL, "%s: the pages are on device %d, the context on %d", who, pages->dev, ctx->dev);
     return D3_OK;
 }

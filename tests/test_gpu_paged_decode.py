@@ -255,3 +255,20 @@ def test_steps_in_any_order_on_pages_that_held_other_rows(order, kv):
         dec.fill_missing_paged(cache, slots, step)
         # fp32 rows differ by the order of sums; an fp16 row that is rounded the other way for that is 2^-11 of itself off
         assert (logits - want[n]).abs().max() < (1e-4 if kv == "f32" else helpers.LOGIT_ATOL), (n, step)
+
+
+def test_rows_go_into_pages_of_a_handle_with_other_query_heads():
+    """Rows know KV heads only: storing and filling need the context's layers, KV heads and head_dim, as documented; a step needs its query heads too."""
+    import torch
+    from paper_2503_08524_amd import D3Error, PagedCache
+    dec = _decoder(GQA, d3_inputs.make_weights(GQA, 0), 1, 32, "f16")
+    dec.set_plan(0.5, 1, 0, 4)
+    tok = dec.prefill(torch.from_numpy(d3_inputs.make_prompt(1, 9, GQA.V, seed=8)).to(DEV))
+    caches = [PagedCache(heads, GQA.H_kv, GQA.hd, 3, 16, 1, 2, n_layers=GQA.L, device=DEV) for heads in (GQA.H, GQA.H_kv)]
+    for cache in caches:
+        _admit(dec, cache, [9])
+        dec.fill_missing_paged(cache, torch.arange(3, 5, dtype=torch.int32, device=DEV), 2)
+    assert torch.equal(caches[0].k_pages, caches[1].k_pages) and torch.equal(caches[0].v_pages, caches[1].v_pages) and caches[0].k_pages.any()
+    with pytest.raises(D3Error) as e:
+        dec.decode_step_paged(caches[1], tok, 1, tok)
+    assert e.value.status == -2 and "heads" in str(e.value)
