@@ -272,3 +272,40 @@ def test_rows_go_into_pages_of_a_handle_with_other_query_heads():
     with pytest.raises(D3Error) as e:
         dec.decode_step_paged(caches[1], tok, 1, tok)
     assert e.value.status == -2 and "heads" in str(e.value)
+
+
+@pytest.mark.parametrize("kv,tight", [("f32", 1e-4), ("f16", helpers.LOGIT_ATOL)])
+def test_a_newcomer_on_recycled_pages_has_the_logits_of_its_own_run(kv, tight):
+    """A sequence takes the place and the pages of one that ended; forced tokens, and its logits in every step are those of the context's own cache, which it has to itself there."""
+    import torch
+    w = d3_inputs.make_weights(GQA, 0)
+    dec = _decoder(GQA, w, 3, 64, kv)
+    dec.set_plan(1.0, 0, 0, 12)
+    lengths = [40, 37, 30]
+    prompts = torch.from_numpy(d3_inputs.make_prompt(3, 40, GQA.V, seed=41)).to(DEV)
+    forced = torch.from_numpy(d3_inputs.make_prompt(12, 3, GQA.V, seed=42)).to(DEV)
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    logits, nxt = torch.zeros(2, GQA.V, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+    cache = _pages(dec, 7, 2, 64)                                  # seven pages for 40 + 8 and 37 + 3 rows: the newcomer's are the ended one's
+    dec.prefill_ragged(prompts, lengths)
+    starts, slots, _ = cache.reserve(ints(40, 37), 77)
+    dec.store_pages(cache, 0, slots[:40])
+    dec.store_pages(cache, 1, slots[40:])
+    former, got = set(cache.tables[1, :3].tolist()), []
+    for i in range(11):
+        if i == 3:
+            starts, slots, _ = cache.reserve(ints(0, -1), 1)
+            starts, slots, _ = cache.reserve(ints(0, 30), 30)
+            assert starts.tolist() == [0, 0, 30] and set(cache.tables[1, :2].tolist()) <= former
+            dec.store_pages(cache, 2, slots)
+        starts, slots, positions = cache.reserve(ints(1, 1), 2)
+        assert positions.tolist() == [40 + i, 37 + i if i < 3 else 30 + i - 3]
+        tok = torch.stack([forced[i, 0], forced[i, 1] if i < 3 else forced[i - 3, 2]])
+        dec.decode_step_paged(cache, tok, 1, nxt, logits=logits, starts=starts)
+        got.append(logits.clone())
+    own = torch.zeros(1, GQA.V, device=DEV)
+    for b, mine in ((0, [x[0] for x in got]), (1, [x[1] for x in got[:3]]), (2, [x[1] for x in got[3:]])):
+        dec.prefill(prompts[b:b + 1, 40 - lengths[b]:].contiguous())
+        for i, x in enumerate(mine):
+            dec.decode_step(forced[i, b:b + 1].contiguous(), i + 1, nxt[:1], logits=own)
+            assert (x - own[0]).abs().max() < tight, (b, i)
