@@ -713,12 +713,16 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                     for (int idx = self; idx < items; idx += 64) some(idx);
                 }
             };
+            // All loads of a round go out together whether there are as many parts or not, so a round is one of three widths.  One sequence, 32 heads, fp16 (four sequences, 8 KV heads of 8, fp32), us by
+            // the width: 2 to 4 parts 4 wide 8.0 (8.6), 5 wide 8.0 (8.7), 8 wide 8.4 (8.9), 16 wide 8.6 (9.6); 5 parts, 4 wide in 16, 8.8 8.2 8.5 8.8 (9.8 8.9 9.0 9.8); 6 to 8 parts, 5 and 8 wide against
+            // 16, 8.2 to 8.4 against 8.7 to 8.9 (9.2 to 9.6 against 10.0 to 10.3); 9 to 16 in two rounds of 8 are up to 0.4 us slower than in one of 16.
             auto join_some = [&](int first, int step, int count, auto done) {
                 typedef std::integral_constant<int, 1> One;
                 typedef std::integral_constant<int, 5> Five;
                 if constexpr (THREADS == 64) join(Five(), One(), first, step, count, done);
                 else if (ITEMS > 1 && items > THREADS) join(std::integral_constant<int, 8>(), std::integral_constant<int, 2>(), first, step, count, done);
-                else if (count <= 5) join(Five(), One(), first, step, count, done);      // (640 rows, 32 heads)
+                else if (count <= 5) join(Five(), One(), first, step, count, done);
+                else if (count <= 8) join(std::integral_constant<int, 8>(), One(), first, step, count, done);
                 else join(std::integral_constant<int, kJoin>(), One(), first, step, count, done);
             };
             const int sets = (parts + kJoin - 1) / kJoin, first = (run - w0) / kJoin * kJoin, count = min(kJoin, parts - first);
