@@ -1,4 +1,5 @@
 // Kernels of the paged cache beside its attention: page tables and slot maps from request lengths, rows into pages, the missing-state fill on pages.
+#include <algorithm>
 #include <type_traits>
 
 #include "pages.h"
@@ -369,11 +370,13 @@ int launch_append_to(const AppendArgs& a, hipStream_t s) {
 }  // namespace
 
 int launch_pages_reserve(const ReserveArgs& a, hipStream_t s) {
-    // Few tokens (a step's): by the same workgroup; many: by a launch of their own over the chip.
-    const bool few = a.max_tokens <= (a.B <= 64 ? 512 : 4096);
-    // One wave for a step of a few sequences, whose pages it can push and pop in a few rounds (8 sequences: 4.3 -> 2.5 us); where there may be many, they need the threads (32 prompts of 2048
-    // rows in pages of 32: 8.1 us, one wave 20).
-    if (few && a.B <= 64 && (long long)a.B * a.max_pages <= 8192) hipLaunchKernelGGL((pages_reserve_kernel<64, 1>), dim3(1), dim3(64), 0, s, a, 1);
+    // Few tokens: by the same workgroup; many: by a launch of their own over the chip.  us by one launch / two: 2048 tokens of 1, 64, 1024 sequences 4.5 / 5.9, 5.7 / 6.8, 6.2 / 7.6; 4096 tokens
+    // 5.1 / 6.0, 7.2 / 6.8, 8.2 / 7.8; a token each of 4096 sequences 11.9 / 13.9, two each 16.5 / 13.8.
+    const bool few = a.max_tokens <= std::max(3500, a.B);
+    // One wave where it has few rounds to go: 1, 8, 64 sequences, us by one wave / a workgroup, a token each 2.1 / 3.9, 2.3 / 4.0, 2.5 / 4.2; 256 tokens in all 2.9 / 4.0, 3.9 / 4.5, 4.3 / 4.2; 512
+    // 3.7 / 4.1, 5.5 / 4.5, 6.6 / 4.3.  Pages that come back cost it a round for 512: full tables of 8192 entries, one of 2, 8, 64 sequences ends 11.1 / 5.2, 4.8 / 4.6, 3.8 / 4.8, all of 1, 8, 64
+    // 19 / 5.5, 22 / 7.3, 25 / 9.0.  A step gains 1.7 us, so four steps or fewer pay for one that ends, ten for all.  Tables of 65536 entries: one ends 73 / 12.9, 22 / 7.7, 5.4 / 5.0, all 136 / 18, 160 / 32, 182 / 46.
+    if (a.B <= 64 && a.max_tokens <= 256 && (long long)a.B * a.max_pages <= 8192) hipLaunchKernelGGL((pages_reserve_kernel<64, 1>), dim3(1), dim3(64), 0, s, a, 1);
     else if (a.B <= 1024) hipLaunchKernelGGL((pages_reserve_kernel<1024, 1>), dim3(1), dim3(1024), 0, s, a, few ? 1 : 0);
     else hipLaunchKernelGGL((pages_reserve_kernel<1024, kPagesMaxSeqs / 1024>), dim3(1), dim3(1024), 0, s, a, few ? 1 : 0);
     hipError_t e = hipGetLastError();

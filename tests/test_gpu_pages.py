@@ -779,3 +779,38 @@ def test_strides_of_dims_with_one_entry_say_nothing():
                  lambda: cache.attend(0, k.transpose(0, 1).contiguous().transpose(0, 1))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("heads,group,hd,kv", [(8, 2, 128, "f16"), (4, 5, 64, "f32"), (2, 17, 128, "f16")])
+def test_attention_of_every_number_of_parts(heads, group, hd, kv):
+    """One sequence of one to twenty chunks, few enough heads for a workgroup to each: as many partial results a head, joined in rounds of every width, and in two rounds."""
+    import torch
+    chunk = 4 * 1024 * 8 // (hd * (2 if kv == "f16" else 4))
+    for parts in range(1, 21):
+        lens = [parts * chunk - parts % 3]
+        cache, g = _cache(lens, heads, group, hd, kv, 16, seed=parts)
+        q = torch.empty(1, heads * group, hd, device=DEV).normal_(generator=g)
+        out = cache.attend(0, q)
+        _check(out, *_reference(cache, q.double(), lens))
+        assert torch.equal(out, cache.attend(0, q))
+
+
+@pytest.mark.parametrize("B,tokens,max_pages", [(3, 256, 60), (3, 257, 60), (3, 257, 4000), (64, 256, 128), (64, 256, 129), (64, 300, 20), (65, 256, 20), (9, 3500, 300), (9, 3501, 300),
+                                                (4000, 4000, 2), (4000, 4001, 2)])
+def test_reserve_on_either_side_of_its_launches(B, tokens, max_pages):
+    """Requests of max_tokens rows and one more where a launch of another form takes over, from tables that are partly full, some of them ending."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    rng = np.random.RandomState(B + tokens)
+    cache = PagedCache(1, 1, 64, B * 2 + tokens // 16 + 70, 16, B, max_pages, device=DEV)
+    rows, tables, stack = [0] * B, cache.tables.tolist(), list(range(cache.n_pages - 1, -1, -1))
+    for step in range(4):
+        cut = np.sort(rng.randint(0, tokens + 1, B - 1)) if B < 1000 else np.arange(1, B)
+        added = np.diff(np.concatenate([[0], cut, [tokens + (step == 2)]]))        # all of max_tokens; then one row too many
+        if step:
+            added[rng.rand(B) < 0.3] = -1
+        want = _reserve_plainly(rows, added.tolist(), tables, stack, 16, max_pages, tokens)
+        starts, slots, positions = cache.reserve(torch.tensor(added, dtype=torch.int32, device=DEV), tokens)
+        rows, tables, stack = want[:3]
+        assert cache.rows.tolist() == rows and cache.tables.tolist() == tables and cache.n_free.tolist() == [len(stack), want[3]] and cache.free_pages[: len(stack)].tolist() == stack
+        assert starts.tolist() == want[4] and slots.tolist() == want[5] and positions.tolist() == want[6]
