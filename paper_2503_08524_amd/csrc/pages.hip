@@ -347,8 +347,11 @@ __global__ __launch_bounds__(256) void pages_fill_kernel(PagesFillArgs a, int la
 
 template <typename T>
 int launch_fill(const PagesFillArgs& a, hipStream_t s) {
-    // enough waves for the chip's latency first, then as many blocks to a wave as can be
-    const int units = a.n * a.H_kv, each = units >= 4096 ? a.n_layers : units >= 512 ? 8 : 4;
+    // Blocks to a wave: one where all of them are few enough to be resident at once (each block is then one store away from its source); where there are more, several, that share their loads.
+    // us by 1, 4, 8, all blocks of a wave, fp16: 8 units 8 blocks 2.2 2.9 3.9 3.8, 80 blocks 2.4 3.1 4.1 22; 32 units 32 blocks 2.6 3.2 4.2 9.9, 80 blocks 3.9 3.8 4.8 22; 128 units 8 blocks 2.6 3.3 4.3
+    // 4.2, 32 blocks 5.2 4.7 5.4 11; 256 units 8 blocks 3.4 3.7 4.7 4.7, 32 blocks 8.0 7.0 7.0 12; 512 units 8 blocks 5.4 4.8 5.5 5.6, 32 blocks 12.5 11.6 10.9 13.3; 1024 units 32 blocks 18.7 20.2 18.8 20.0;
+    // 4096 units 32 blocks 95.8 100.4 100.4 99.3; 16384 units 32 blocks 520 516 520 510, 80 blocks 1285 1275 1286 1253.
+    const int units = a.n * a.H_kv, each = (long long)units * a.n_layers <= 2048 ? 1 : units >= 4096 ? a.n_layers : units >= 512 ? 8 : 4;
     const dim3 grid((units + 3) / 4, (a.n_layers + each - 1) / each);
     if (a.hd == 64) hipLaunchKernelGGL((pages_fill_kernel<T, 64>), grid, dim3(256), 0, s, a, each);
     else hipLaunchKernelGGL((pages_fill_kernel<T, 128>), grid, dim3(256), 0, s, a, each);

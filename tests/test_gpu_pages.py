@@ -814,3 +814,23 @@ def test_reserve_on_either_side_of_its_launches(B, tokens, max_pages):
         rows, tables, stack = want[:3]
         assert cache.rows.tolist() == rows and cache.tables.tolist() == tables and cache.n_free.tolist() == [len(stack), want[3]] and cache.free_pages[: len(stack)].tolist() == stack
         assert starts.tolist() == want[4] and slots.tolist() == want[5] and positions.tolist() == want[6]
+
+
+@pytest.mark.parametrize("n,heads,layers", [(16, 2, 64), (16, 2, 65), (1, 2, 79), (64, 8, 4), (64, 8, 9), (63, 8, 5), (512, 8, 3), (511, 8, 11), (300, 1, 6), (2048, 1, 1)])
+@pytest.mark.parametrize("kv", ["f16", "f32"])
+def test_fill_on_either_side_of_its_shares(n, heads, layers, kv):
+    """As many rows and blocks as a wave is given one block, four, eight or all of them, and one more."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    g = torch.Generator(device=DEV)
+    g.manual_seed(n + layers)
+    cache = PagedCache(heads, heads, 64, n // 16 + 2, 16, 1, 1, kv_dtype=kv, n_layers=layers + 2, device=DEV)
+    cache.k_pages.normal_(generator=g)
+    cache.v_pages.normal_(generator=g)
+    slots = torch.randperm(cache.n_pages * 16, generator=g, device=DEV)[:n]
+    want = [_as_rows(cache, p) for p in (cache.k_pages, cache.v_pages)]
+    for rows in want:
+        rows[1:layers + 1, slots] = rows[layers + 1, slots][None]
+    cache.fill(slots.int(), layers + 1, 1, layers)
+    for rows, p in zip(want, (cache.k_pages, cache.v_pages)):
+        assert torch.equal(rows, _as_rows(cache, p))
