@@ -289,7 +289,8 @@ int d3_pages_live(d3_pages *pages, int32_t B, const int32_t *rows, const int32_t
  * Given, they are row rows[b] - 1 of every sequence that has rows, which the call also writes to its page (which no other sequence of the call may list); else that row is there already.
  * The call cannot tell a sequence that a reserve refused, or that asked for nothing: it would lose its newest row, so `rows` is then d3_pages_live's.  rope_cs: dev float [B][head_dim / 2][2]: q and
  * k_new turn by it; NULL: neither does.  q, k_new, v_new, rope_cs 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
- * out may be q itself.  Keys and values are used as the pool holds them; sums and softmax in 32 bits. */
+ * out may be q itself.  Keys and values are used as the pool holds them; sums, maxima and partial results are in 32 bits.  Into the products q and the weights go in fp32 with D3_F32 pools, as
+ * the sum of two fp16 halves (22 bits) with D3_F16 pools.  A row whose score is -infinity has the weight 0; out is 0 too where every row's is. */
 int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,
                        int64_t kv_stride, const float *rope_cs, const int32_t *tables, const int32_t *rows, float scale, void *out,
                        int64_t out_stride, void *hip_stream);

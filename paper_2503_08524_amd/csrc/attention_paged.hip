@@ -15,9 +15,9 @@
 // So the head stays with lane % 16 throughout, the running maximum and sum of a softmax are the lane's own, and of what is read or weighed nothing passes through LDS before the
 // four waves of a workgroup are merged at the end of a run (q does, once, to leave the registers to the rows in flight: 16 loads of 16 bytes a lane).
 //
-// Bound by memory where there is much of it: 32 x 2304 rows of 32 heads, fp16, 191 us = 6.3 TB/s (a pure read 6.7); 48 requests of 1 to 32768 rows of 8 heads 110 us, 5.9 TB/s.  Matrix
+// Bound by memory where there is much of it: 32 x 2304 rows of 32 heads, fp16, 189 us = 6.4 TB/s (a pure read 6.7); 48 requests of 1 to 32768 rows of 8 heads 109 us, 6.0 TB/s.  Matrix
 // and vector units are at 8 and 13 % there, so one form serves 1 to 16 query heads a KV head and both types.  Small launches are a chain of round trips: one row 5.5 us, 640 rows of 32 heads, five
-// runs a head, 9.3 us: lengths 0.4, place found 0.3, tables and q 1.4, rows 1.7, turn 0.7, merge 0.7, publish, arrive and join 2.4.
+// runs a head, 9.2 us: lengths 0.4, place found 0.3, tables and q 1.4, rows 1.7, turn 0.7, merge 0.7, publish, arrive and join 2.4.
 #include <algorithm>
 #include <type_traits>
 

@@ -10,7 +10,7 @@ namespace {
 
 // ---------------- page tables and slot maps ----------------
 // One workgroup: sums over the sequences (a wave's by row shifts, no LDS; the waves' through LDS), then pages and tokens found in those sums by bisection.  A chain of round trips
-// bounds it: requests in, sums, pages of the stack, tables, slots (8 sequences 2.4 us, 256 with 20000 new rows 6.2 and 3.7 for the slots).
+// bounds it: requests in, sums, pages of the stack, tables, slots (8 sequences 2.5 us, 256 with 20000 new rows 6.2 and 3.4 for the slots).
 __device__ __forceinline__ unsigned long long shifted64(unsigned long long v, int which) {
     unsigned lo, hi;
 #define D3_SHIFT(ctrl, rows) lo = __builtin_amdgcn_update_dpp(0, (unsigned)v, ctrl, rows, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (unsigned)(v >> 32), ctrl, rows, 0xf, false)
@@ -316,7 +316,7 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs a) {
 
 // ---------------- missing-state fill on pages ----------------
 // A wave has one (token, KV head): 16 bytes of the key in the first lanes, one or two elements of the value in each, read once from the source block
-// and written into a few of the dropped ones (grid.y).  40 blocks of 8 rows of 8 heads, fp32, 4.7 us: little more than a launch, though the values, four bytes in every 16, write 6.5 MB
+// and written into a few of the dropped ones (grid.y).  40 blocks of 8 rows of 8 heads, fp32, 4.5 us: little more than a launch, though the values, four bytes in every 16, write 6.5 MB
 // for 2.6.
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void pages_fill_kernel(PagesFillArgs a, int layers_each) {

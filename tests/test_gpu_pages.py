@@ -834,3 +834,33 @@ def test_fill_on_either_side_of_its_shares(n, heads, layers, kv):
     cache.fill(slots.int(), layers + 1, 1, layers)
     for rows, p in zip(want, (cache.k_pages, cache.v_pages)):
         assert torch.equal(rows, _as_rows(cache, p))
+
+
+@pytest.mark.parametrize("lens", [[50, 300, 7], [1, 64, 65], [9000, 20, 40]])
+def test_attention_of_scores_of_minus_infinity(lens):
+    """Keys of -infinity where the query is positive: such rows weigh nothing, wherever they stand in a tile or a run; where all rows of a sequence are such, its outputs are 0."""
+    import torch
+    cache, g = _cache(lens, 2, 2, 64, "f32", 16, seed=16)
+    q = torch.empty(3, 4, 64, device=DEV).normal_(generator=g)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.1
+    rows = _as_rows(cache, cache.k_pages)
+    gone = [torch.rand(n, generator=g, device=DEV) < 0.5 for n in lens]
+    gone[0][: lens[0] // 2] = True
+    gone[2][:] = True
+    for b, n in enumerate(lens):
+        rows[0, _slots(cache, b, range(n))[gone[b]], :, 0] = -math.inf
+    _from_rows(cache, cache.k_pages, rows)
+    out = cache.attend(0, q)
+    K, V = (_as_rows(cache, p)[0].double() for p in (cache.k_pages, cache.v_pages))
+    for b, n in enumerate(lens):
+        at = _slots(cache, b, range(n))[~gone[b]]
+        if not len(at):
+            assert not out[b].any()
+            continue
+        k, v = K[at].repeat_interleave(2, 1), V[at].repeat_interleave(2, 1)
+        s = torch.einsum("hd,nhd->hn", q[b].double(), k) / 8
+        want = torch.einsum("hn,nhd->hd", torch.softmax(s, -1), v)
+        # as in _reference: 64 products summed in fp32 and their roundings, twice in a weight, and the sums over n rows
+        size = torch.einsum("hd,nhd->hn", q[b].double().abs(), k.abs()).max() / 8
+        most = v.abs().max() * (2 * (2.0 ** -22 + 69 * 2.0 ** -24) * size + 2.0 ** -21 + (n / 8 + 64) * 2.0 ** -24)
+        assert (out[b].double() - want).abs().max() <= most
