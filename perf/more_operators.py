@@ -1,0 +1,441 @@
+"""Performance cases of a paged key-value cache held in 8 bits: rows quantised as they are written, read back, copied between blocks, and attended over.
+
+    listed(), draw(rng)   the cases, and more of the same ranges
+    prepare(case, seed)   inputs, page pools and page tables on the GPU, as a program has them before the call
+    run(state)            one pass through an operator; its outputs, and the pools it wrote
+    work(case)            bytes and flops a pass cannot do without
+    exact(case, seed)     the same outputs in float64, by the definition
+
+With `own` false, run() computes the operators by elementary torch operations, in 32 bits; with `own` true it calls `binding.PagedCache`.
+
+A row of a head (a key after its rotation, or a value) is held as codes and one fp32 scale: with a its largest magnitude and Q the largest code (127 for "i8", integers; 448 for "f8",
+the e4m3 type), scale = a / Q and code = x * (Q / a), rounded to nearest even; it stands for code * scale.
+The pools: a page holds `page_rows` rows of every key-value head.  Keys [layer][page][head][row][dim]; values [layer][page][head][row / 16][dim][row % 16]; scales of either
+[layer][page][head][row].  A slot is page * page_rows + row.
+
+Pools of "f8" are returned as they are (their codes are floating-point values, in units of the scales beside them).  Where "i8" codes are computed, the pass reads the rows back
+and their values are returned.
+"""
+import math
+from types import SimpleNamespace
+
+import torch
+
+own = False
+
+DEVICE = "cuda:0"
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i8": torch.int8, "f8": torch.float8_e4m3fn}
+BYTES = {"f32": 4, "f16": 2, "bf16": 2}
+MOST_CODE = {"i8": 127.0, "f8": 448.0}
+UNIT = 16                 # rows of a value's dim that lie side by side
+ROPE_BASE = 10000.0
+MOST, LEAST = 3e38, 2.0 ** -100       # a row's magnitude as its scale counts it; below the least a row is held as zeros
+
+
+def _append(name, layers, tokens, heads, hd, src, kv, page_rows, rope):
+    """Into "f8" pools; into "i8" pools the rows are read back too (a prompt's next piece attends over what the cache holds)."""
+    return {"name": name, "op": "append" if kv == "f8" else "store", "layers": layers, "tokens": tokens, "heads": heads, "hd": hd, "src": src, "kv": kv,
+            "page_rows": page_rows, "rope": rope}
+
+
+def _read(name, layers, tokens, heads, hd, to, kv, page_rows):
+    return {"name": name, "op": "read", "layers": layers, "tokens": tokens, "heads": heads, "hd": hd, "src": to, "kv": kv, "page_rows": page_rows}
+
+
+def _fill(name, layers, dropped, B, heads, hd, page_rows):
+    return {"name": name, "op": "fill", "layers": layers, "dropped": dropped, "B": B, "heads": heads, "hd": hd, "kv": "f8", "page_rows": page_rows}
+
+
+def _attend(name, B, rows, spread, heads, group, hd, act, kv, page_rows, new):
+    return {"name": name, "op": "attend", "B": B, "rows": rows, "spread": spread, "heads": heads, "group": group, "hd": hd, "act": act,
+            "kv": kv, "page_rows": page_rows, "new": new}
+
+
+def listed():
+    return [
+        # a prompt's keys and values of one block, rotated and quantised on their way into pages (7B widths)
+        _append("append_prompt_7b", 1, 512, 32, 128, "f32", "f8", 16, True),
+        # the rows of a whole prompt pass moved into pages, several blocks in one call (70B widths, fp32 rows)
+        _append("append_blocks_70b", 8, 1024, 8, 128, "f32", "f8", 64, False),
+        # a piece of a prompt of odd length from a bf16 model, head_dim 64, and what the cache holds of it
+        _append("store_piece_odd", 1, 77, 8, 64, "bf16", "i8", 16, True),
+        # a long prompt of one block and what the cache holds of it (13B widths, fp16 rows)
+        _append("store_prompt_13b", 1, 1024, 40, 128, "f16", "i8", 16, True),
+        # a short sequence out of its pages, bf16, head_dim 64
+        _read("read_rows_odd", 1, 333, 8, 64, "bf16", "f8", 16),
+        # a long sequence that leaves the pages: several blocks in one call (7B widths)
+        _read("read_sequence_7b", 4, 2304, 32, 128, "f16", "i8", 32),
+        # the blocks that a step dropped get the row of the last block that ran: one user
+        _fill("fill_7b_b1", 32, 15, 1, 32, 128, 16),
+        # the same of a batch and a deep model
+        _fill("fill_70b_b8", 80, 40, 8, 8, 128, 64),
+        # one user's step, nothing but latency (7B widths)
+        _attend("attend_7b_b1", 1, 640, "equal", 32, 1, 128, "f32", "f8", 16, True),
+        # grouped queries (70B widths, batch 8), rows written before
+        _attend("attend_70b_b8", 8, 1152, "equal", 8, 8, 128, "f32", "i8", 64, False),
+        # requests of all ages, one to 32768 rows, some places empty; a bf16 model's queries, rows written before
+        _attend("attend_ragged_b48", 48, 32768, "log", 8, 4, 128, "bf16", "i8", 16, False),
+        # the full batch with long contexts: the largest stream of cache rows (7B widths, batch 32)
+        _attend("attend_7b_b32", 32, 2304, "equal", 32, 1, 128, "f32", "f8", 32, True),
+    ]
+
+
+def _between(rng, lo, hi):
+    """An integer spread over the logarithm of [lo, hi]."""
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    case = _drawn(rng)
+    del case["name"]
+    return case
+
+
+def _drawn(rng):
+    op = rng.choice(["append", "read", "fill", "attend", "attend"])
+    page_rows = rng.choice([16, 16, 32, 64, 128])
+    hd = rng.choice([64, 128, 128])
+    kv = rng.choice(["i8", "f8"])
+    if op in ("append", "read"):
+        heads, layers = rng.choice([1, 2, 4, 5, 8, 32, 40]), rng.choice([1, 1, 2, 5])
+        tokens = _between(rng, 1, min(6000, (1 << 26) // (heads * hd * layers)))
+        kind = rng.choice(["f32", "bf16", "f16"])
+        if op == "read":
+            return _read("", layers, tokens, heads, hd, kind, kv, page_rows)
+        return _append("", layers, tokens, heads, hd, kind, kv, page_rows, rng.random() < 0.5)
+    if op == "fill":
+        layers = rng.choice([4, 32, 40, 80])
+        heads = rng.choice([2, 4, 8, 40 if layers == 40 else 32])
+        most = min(32, max(1, (1 << 29) // (layers * heads * page_rows * hd)))
+        return _fill("", layers, rng.randint(1, layers - 1), _between(rng, 1, most), heads, hd, page_rows)
+    B = _between(rng, 1, 96)
+    group = rng.choice([1, 1, 2, 3, 4, 5, 7, 8, 16, 20])
+    heads = rng.choice([1, 2, 4, 8, 32] if group <= 4 else [1, 2, 8])
+    most = max(16, min(32768, 540000000 // (B * heads * hd * 2 * max(1, group // 4))))
+    return _attend("", B, _between(rng, 1, most), rng.choice(["equal", "log"]), heads, group, hd, rng.choice(["f32", "bf16", "f16"]), kv,
+                   page_rows, kv == "f8" and rng.random() < 0.7)
+
+
+def _lengths(case):
+    """Rows of every sequence: all alike, or from 1 to case["rows"] evenly over the logarithm in a fixed mixed order, every 16th of 16 or more none."""
+    B, rows = case["B"], case["rows"]
+    if case["spread"] == "equal":
+        return [rows] * B
+    n = [max(1, round(rows ** ((i + 1) / B))) for i in range(B)]
+    step = next(s for s in (37, 41, 43, 47, 53, 59, 61, 67) if math.gcd(s, B) == 1)
+    return [0 if B >= 16 and b % 16 == 5 else n[b * step % B] for b in range(B)]
+
+
+def _pages(rows, page_rows):
+    return -(-rows // page_rows)
+
+
+def _generator(seed):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(int(seed))
+    return g
+
+
+def _pools(s, g, layers, n_pages, heads, page_rows, hd, kv):
+    """Pools as rows of normal values leave them: the largest of a row's dims lies 2 to 4 deviations out."""
+    def one(dims):
+        x = torch.empty(dims, dtype=torch.float16, device=DEVICE).normal_(0, MOST_CODE[kv] / 3.5, generator=g).clamp_(-MOST_CODE[kv], MOST_CODE[kv])
+        return (x.round() if kv == "i8" else x).to(TYPES[kv])
+    s.k_pages, s.v_pages = one((layers, n_pages, heads, page_rows, hd)), one((layers, n_pages, heads, page_rows // UNIT, hd, UNIT))
+    s.k_scales, s.v_scales = (torch.empty(layers, n_pages, heads, page_rows, device=DEVICE).uniform_(2 / MOST_CODE[kv], 4 / MOST_CODE[kv], generator=g) for _ in range(2))
+
+
+def _angles(positions, hd):
+    """(cos, sin) of the rotary angles of the given positions: [n][hd / 2][2], from 64 bits."""
+    inv = ROPE_BASE ** (-2.0 * torch.arange(hd // 2, dtype=torch.float64, device=DEVICE) / hd)
+    a = positions.double()[:, None] * inv
+    return torch.stack([a.cos(), a.sin()], -1).float().contiguous()
+
+
+def prepare(case, seed):
+    g = _generator(seed)
+    s = SimpleNamespace(case=case)
+    pr, op, kv, hd, heads = case["page_rows"], case["op"], case["kv"], case["hd"], case["heads"]
+    layers, group = case.get("layers", 1), case.get("group", 1)
+    ints = dict(dtype=torch.int32, device=DEVICE)
+    if op == "attend":
+        B = case["B"]
+        n = _lengths(case)
+        s.max_pages = max(1, _pages(max(n), pr))
+        s.n_pages = sum(_pages(x, pr) for x in n) + 8
+        s.rows = torch.tensor(n, **ints)
+        s.tables = torch.full((B, s.max_pages), -1, **ints)
+        at = torch.arange(s.max_pages, device=DEVICE)[None] < ((s.rows + pr - 1) // pr)[:, None]
+        s.tables[at] = torch.randperm(s.n_pages, generator=g, device=DEVICE).int()[: int(at.sum())]
+        act = dict(dtype=TYPES[case["act"]], device=DEVICE)
+        s.q = torch.empty(B, heads * group, hd, **act).normal_(generator=g)
+        s.k = s.v = s.rope_cs = None
+        if case["new"]:
+            s.k = torch.empty(B, heads, hd, **act).normal_(generator=g)
+            s.v = torch.empty(B, heads, hd, **act).normal_(generator=g)
+            s.rope_cs = _angles((s.rows - 1).clamp(min=0), hd)
+        s.out = torch.empty_like(s.q)
+    else:
+        n = case["B"] if op == "fill" else case["tokens"]
+        s.n_pages = n + 2 if op == "fill" else _pages(n + 5, pr) + 2
+        order = torch.randperm(s.n_pages, generator=g, device=DEVICE).int()
+        if op == "fill":                                   # the newest row of every sequence
+            s.slots = order[:n] * pr + torch.randint(0, pr, (n,), generator=g, device=DEVICE).int()
+        else:                                              # consecutive rows of one sequence that holds 5 already
+            p = torch.arange(5, n + 5, device=DEVICE)
+            s.slots = order[p // pr] * pr + (p % pr).int()
+            rows = dict(dtype=TYPES[case["src"]], device=DEVICE)
+            if op != "read":
+                s.k = torch.empty(layers, n, heads, hd, **rows).normal_(generator=g)
+                s.v = torch.empty(layers, n, heads, hd, **rows).normal_(generator=g)
+                s.rope_cs = _angles(p, hd) if case["rope"] else None
+            if op != "append":
+                s.k_out, s.v_out = (torch.empty(layers, n, heads, hd, **rows) for _ in range(2))
+    _pools(s, g, layers, s.n_pages, heads, pr, hd, kv)
+    if own:
+        from paper_2503_08524_amd import binding
+        more = dict(tables=s.tables, rows=s.rows, max_batch=case["B"], max_pages=s.max_pages) if op == "attend" else dict(max_batch=1, max_pages=1)
+        s.cache = binding.PagedCache(heads * group, heads, hd, s.n_pages, pr, kv_dtype=kv, n_layers=layers, k_pages=s.k_pages,
+                                     v_pages=s.v_pages, k_scales=s.k_scales, v_scales=s.v_scales, device=DEVICE, **more)
+    return s
+
+
+def _window(case):
+    """(source block, first dropped block) of a fill: the window begins at 0.6 of the depth, or where it still fits."""
+    first = min(int(0.6 * case["layers"]), case["layers"] - case["dropped"])
+    return (first - 1 if first > 0 else case["dropped"]), first
+
+
+def _held(s):
+    return {"k": s.k_pages, "v": s.v_pages, "k_scales": s.k_scales, "v_scales": s.v_scales}
+
+
+def run(s):
+    case, op = s.case, s.case["op"]
+    if own:
+        if op in ("append", "store"):
+            s.cache.append(0, s.slots, s.k, s.v, rope_cs=s.rope_cs)
+        if op in ("store", "read"):
+            s.cache.read(0, s.slots, s.k_out, s.v_out)
+        if op == "fill":
+            src, first = _window(case)
+            s.cache.fill(s.slots, src, first, case["dropped"])
+        if op == "attend":
+            s.cache.attend(0, s.q, s.k, s.v, rope_cs=s.rope_cs, out=s.out)
+    else:
+        _plain[op](s)
+    if op == "read":
+        return {"k": s.k_out, "v": s.v_out}
+    if op == "store":
+        return {"k": s.k_out, "v": s.v_out, "k_scales": s.k_scales, "v_scales": s.v_scales}
+    if op == "attend":
+        return {"out": s.out, **_held(s)} if case["new"] else {"out": s.out}
+    return _held(s)
+
+
+# ---------------- the plain forms ----------------
+
+def _rotated(x, cs):
+    """x [..., n, heads, hd] turned by cs [n][hd / 2][2]: dims j and j + hd / 2 together."""
+    half = x.shape[-1] // 2
+    c, n = cs[:, None, :, 0], cs[:, None, :, 1]
+    a, b = x[..., :half], x[..., half:]
+    return torch.cat([a * c - b * n, b * c + a * n], -1)
+
+
+def _quantised(x, kv):
+    """(codes, scales) of rows x [..., hd]."""
+    a = x.abs().amax(-1, keepdim=True).clamp(max=MOST)
+    most = torch.full_like(a, MOST_CODE[kv])               # (a tensor: torch multiplies by the reciprocal of a number)
+    zeros = a < LEAST
+    y = (x * torch.where(zeros, 0, most / a)).clamp(-MOST_CODE[kv], MOST_CODE[kv])
+    return (y.round() if kv == "i8" else y).to(TYPES[kv]), torch.where(zeros, 0, a / most)[..., 0]
+
+
+def _bits(pool):
+    return pool.view(torch.uint8)
+
+
+def _put(s, slots, k, v):
+    """k, v [layers][n][heads][hd] into the rows `slots` of the pools."""
+    pr = s.case["page_rows"]
+    page, row = (slots // pr).long(), (slots % pr).long()
+    (kc, ks), (vc, vs) = _quantised(k, s.case["kv"]), _quantised(v, s.case["kv"])
+    _bits(s.k_pages)[:, page, :, row] = _bits(kc).transpose(0, 1)
+    _bits(s.v_pages)[:, page, :, row // UNIT, :, row % UNIT] = _bits(vc).transpose(0, 1)
+    s.k_scales[:, page, :, row], s.v_scales[:, page, :, row] = ks.transpose(0, 1), vs.transpose(0, 1)
+
+
+def _plain_append(s):
+    k = s.k.float()
+    _put(s, s.slots, _rotated(k, s.rope_cs) if s.rope_cs is not None else k, s.v.float())
+
+
+def _plain_read(s):
+    pr, kv = s.case["page_rows"], TYPES[s.case["kv"]]
+    page, row = (s.slots // pr).long(), (s.slots % pr).long()
+    k = _bits(s.k_pages)[:, page, :, row].view(kv).float() * s.k_scales[:, page, :, row][..., None]            # [n][layers][heads][hd]
+    v = _bits(s.v_pages)[:, page, :, row // UNIT, :, row % UNIT].view(kv).float() * s.v_scales[:, page, :, row][..., None]
+    s.k_out.copy_(k.transpose(0, 1))
+    s.v_out.copy_(v.transpose(0, 1))
+
+
+def _plain_store(s):
+    _plain_append(s)
+    _plain_read(s)
+
+
+def _plain_fill(s):
+    pr = s.case["page_rows"]
+    src, first = _window(s.case)
+    last = first + s.case["dropped"]
+    page, row = (s.slots // pr).long(), (s.slots % pr).long()
+    k, v = _bits(s.k_pages), _bits(s.v_pages)
+    k[first:last, page, :, row] = k[src, page, :, row][:, None]
+    v[first:last, page, :, row // UNIT, :, row % UNIT] = v[src, page, :, row // UNIT, :, row % UNIT][:, None]
+    s.k_scales[first:last, page, :, row] = s.k_scales[src, page, :, row][:, None]
+    s.v_scales[first:last, page, :, row] = s.v_scales[src, page, :, row][:, None]
+
+
+def _plain_attend(s):
+    case = s.case
+    B, pr, hd, heads, group, kv = case["B"], case["page_rows"], case["hd"], case["heads"], case["group"], TYPES[case["kv"]]
+    q = s.q.float()
+    rows = s.rows.long()
+    if case["new"]:
+        q = _rotated(q, s.rope_cs)
+        last = (rows - 1).clamp(min=0)
+        slots = s.tables.gather(1, (last // pr)[:, None])[:, 0].long() * pr + last % pr
+        live = rows > 0
+        _put(s, slots[live], _rotated(s.k.float(), s.rope_cs)[live][None], s.v.float()[live][None])
+    t = torch.arange(case["rows"], device=DEVICE)
+    page = s.tables[:, t // pr].clamp(min=0).long()        # [B][rows]
+    k = _bits(s.k_pages)[0][page, :, t % pr].view(kv).float() * s.k_scales[0][page, :, t % pr][..., None]      # [B][rows][heads][hd]
+    v = _bits(s.v_pages)[0][page, :, (t % pr) // UNIT, :, t % UNIT].view(kv).float() * s.v_scales[0][page, :, t % pr][..., None]
+    score = torch.matmul(q.view(B, heads, group, hd), k.permute(0, 2, 3, 1).contiguous()) / math.sqrt(hd)
+    dead = (t[None] >= rows[:, None])[:, None, None]
+    score = score.masked_fill(dead, -math.inf)
+    top = score.amax(-1, keepdim=True).clamp(min=torch.finfo(torch.float32).min)
+    p = torch.exp(score - top)
+    total = p.sum(-1, keepdim=True)
+    out = torch.matmul(p, v.permute(0, 2, 1, 3).contiguous()) / torch.where(total > 0, total, 1)
+    s.out.copy_(out.view(B, heads * group, hd))
+
+
+_plain = {"append": _plain_append, "store": _plain_store, "read": _plain_read, "fill": _plain_fill, "attend": _plain_attend}
+
+
+# ---------------- 64 bits ----------------
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"append": _exact_append, "store": _exact_append, "read": _exact_read, "fill": _exact_fill, "attend": _exact_attend}[case["op"]](s)
+
+
+def _turn(x, positions):
+    """The rotation by its definition: x [n][heads][hd] double, angles from the positions."""
+    hd = x.shape[-1]
+    j = torch.arange(hd // 2, dtype=torch.float64, device=x.device)
+    z = torch.complex(x[..., : hd // 2], x[..., hd // 2:]) * torch.polar(torch.ones_like(j), positions.double()[:, None] / ROPE_BASE ** (2 * j / hd))[:, None]
+    return torch.cat([z.real, z.imag], -1)
+
+
+def _nearest(x, kv):
+    """(codes, scales) of rows x [..., hd] in double: whole numbers, or steps of 2^-3 of a power of two, none below 2^-9."""
+    scale = x.abs().max(-1).values / MOST_CODE[kv]
+    y = x / scale[..., None]
+    if kv == "i8":
+        return torch.round(y), scale
+    step = torch.exp2(torch.floor(torch.log2(y.abs().clamp(min=2.0 ** -6))) - 3)
+    return torch.round(y / step) * step, scale
+
+
+def _exact_append(s):
+    case = s.case
+    pr, kv, n = case["page_rows"], case["kv"], s.slots.numel()
+    at, slots = torch.arange(5, 5 + n, device=DEVICE), s.slots.long()
+    pools = [s.k_pages.double(), s.v_pages.double(), s.k_scales.double(), s.v_scales.double()]
+    held = [[], []]
+    for l in range(case["layers"]):
+        k = s.k[l].double()
+        for i, x in enumerate([_turn(k, at) if case["rope"] else k, s.v[l].double()]):
+            codes, scale = _nearest(x, kv)
+            held[i].append(codes * scale[..., None])
+            if i == 0:
+                pools[0][l][slots // pr, :, slots % pr] = codes
+            else:
+                pools[1][l][slots // pr, :, slots % pr // UNIT, :, slots % UNIT] = codes
+            pools[2 + i][l][slots // pr, :, slots % pr] = scale
+    if case["op"] == "store":
+        return {"k": torch.stack(held[0]), "v": torch.stack(held[1]), "k_scales": pools[2], "v_scales": pools[3]}
+    return {"k": pools[0], "v": pools[1], "k_scales": pools[2], "v_scales": pools[3]}
+
+
+def _exact_read(s):
+    pr, slots = s.case["page_rows"], s.slots.long()
+    k, v = [], []
+    for l in range(s.case["layers"]):
+        scales = [p[l].double()[slots // pr, :, slots % pr] for p in (s.k_scales, s.v_scales)]
+        k.append(s.k_pages[l].double()[slots // pr, :, slots % pr] * scales[0][..., None])
+        v.append(s.v_pages[l].double()[slots // pr, :, slots % pr // UNIT, :, slots % UNIT] * scales[1][..., None])
+    return {"k": torch.stack(k), "v": torch.stack(v)}
+
+
+def _exact_fill(s):
+    pr = s.case["page_rows"]
+    src, first = _window(s.case)
+    k, v = s.k_pages.double(), s.v_pages.double()
+    for l in range(first, first + s.case["dropped"]):
+        for slot in s.slots.tolist():
+            page, row = divmod(slot, pr)
+            k[l, page, :, row] = k[src, page, :, row]
+            v[l, page, :, row // UNIT, :, row % UNIT] = v[src, page, :, row // UNIT, :, row % UNIT]
+            s.k_scales[l, page, :, row] = s.k_scales[src, page, :, row]
+            s.v_scales[l, page, :, row] = s.v_scales[src, page, :, row]
+    return {"k": k, "v": v, "k_scales": s.k_scales.double(), "v_scales": s.v_scales.double()}
+
+
+def _exact_attend(s):
+    case = s.case
+    pr, hd, heads, group, kv = case["page_rows"], case["hd"], case["heads"], case["group"], case["kv"]
+    out = torch.zeros(s.q.shape, dtype=torch.float64, device=DEVICE)
+    pools = [p.double() for p in (s.k_pages, s.v_pages, s.k_scales, s.v_scales)] if case["new"] else None
+    for b, n in enumerate(s.rows.tolist()):
+        if n == 0:
+            continue
+        pages = s.tables[b, : _pages(n, pr)].long()
+        ks, vs = (p[0][pages].permute(0, 2, 1).reshape(-1, heads)[:n, :, None].double() for p in (s.k_scales, s.v_scales))
+        k = _bits(s.k_pages)[0][pages].view(TYPES[kv]).permute(0, 2, 1, 3).reshape(-1, heads, hd)[:n].double() * ks
+        v = _bits(s.v_pages)[0][pages].view(TYPES[kv]).permute(0, 2, 4, 1, 3).reshape(-1, heads, hd)[:n].double() * vs
+        q = s.q[b].double()
+        if case["new"]:
+            at = torch.tensor([n - 1], device=DEVICE)
+            q = _turn(q[None], at)[0]
+            (kc, ks), (vc, vs) = _nearest(_turn(s.k[b:b + 1].double(), at)[0], kv), _nearest(s.v[b].double(), kv)
+            k[-1], v[-1] = kc * ks[:, None], vc * vs[:, None]
+            page, row = int(pages[-1]), (n - 1) % pr
+            pools[0][0, page, :, row], pools[1][0, page, :, row // UNIT, :, row % UNIT] = kc, vc
+            pools[2][0, page, :, row], pools[3][0, page, :, row] = ks, vs
+        score = torch.bmm(q.view(heads, group, hd), k.permute(1, 2, 0).contiguous()) / math.sqrt(hd)
+        out[b] = torch.bmm(torch.softmax(score, -1), v.permute(1, 0, 2).contiguous()).view(heads * group, hd)
+    return {"out": out, "k": pools[0], "v": pools[1], "k_scales": pools[2], "v_scales": pools[3]} if case["new"] else {"out": out}
+
+
+def work(case):
+    op = case["op"]
+    values = case["heads"] * case["hd"] * 2                # of a row
+    held = values + case["heads"] * 2 * 4                  # bytes of a row: codes and scales
+    if op == "fill":
+        return {"bytes": case["B"] * (4 + held * (1 + case["dropped"])), "flops": 0}
+    if op == "attend":
+        n, heads = sum(_lengths(case)), case["heads"] * case["group"]
+        act = case["B"] * BYTES[case["act"]] * (2 * heads * case["hd"] + (values if case["new"] else 0))
+        return {"bytes": n * held + act, "flops": 4 * n * heads * case["hd"]}
+    n = case["tokens"] * case["layers"]
+    bytes_ = n * (held + values * BYTES[case["src"]]) + 4 * case["tokens"]
+    if op == "read":
+        return {"bytes": bytes_, "flops": n * values}
+    if op == "store":                                      # the values that were just held, read back
+        bytes_ += n * values * BYTES[case["src"]]
+    # a magnitude, a product and a rounding a value, and the rotation of half of them
+    return {"bytes": bytes_ + (case["tokens"] * case["hd"] * 4 if case["rope"] else 0), "flops": n * values * 3 + (n * values * 3 // 2 if case["rope"] else 0)}
