@@ -8,12 +8,12 @@
 
 With `own` false, run() computes the operators by elementary torch operations, in 32 bits; with `own` true it calls `binding.PagedCache`.
 
-A row of a head (a key after its rotation, or a value) is held as codes and one fp32 scale: with a its largest magnitude and Q the largest code (127 for "i8", integers; 448 for "f8",
-the e4m3 type), scale = a / Q and code = x * (Q / a), rounded to nearest even; it stands for code * scale.
+A row of a head (a key after its rotation, or a value) is held as codes and one fp32 scale: with a its largest magnitude and Q the largest code (127 for "i8", whole numbers; 448 for "e4m3",
+the floating-point type), scale = a / Q and code = x * (Q / a), rounded to nearest even; it stands for code * scale.
 The pools: a page holds `page_rows` rows of every key-value head.  Keys [layer][page][head][row][dim]; values [layer][page][head][row / 16][dim][row % 16]; scales of either
 [layer][page][head][row].  A slot is page * page_rows + row.
 
-Pools of "f8" are returned as they are (their codes are floating-point values, in units of the scales beside them).  Where "i8" codes are computed, the pass reads the rows back
+Pools of "e4m3" are returned as they are (their codes are floating-point values, in units of the scales beside them).  Where "i8" codes are computed, the pass reads the rows back
 and their values are returned.
 """
 import math
@@ -24,17 +24,17 @@ import torch
 own = False
 
 DEVICE = "cuda:0"
-TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i8": torch.int8, "f8": torch.float8_e4m3fn}
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16, "i8": torch.int8, "e4m3": torch.float8_e4m3fn}
 BYTES = {"f32": 4, "f16": 2, "bf16": 2}
-MOST_CODE = {"i8": 127.0, "f8": 448.0}
+MOST_CODE = {"i8": 127.0, "e4m3": 448.0}
 UNIT = 16                 # rows of a value's dim that lie side by side
 ROPE_BASE = 10000.0
 MOST, LEAST = 3e38, 2.0 ** -100       # a row's magnitude as its scale counts it; below the least a row is held as zeros
 
 
 def _append(name, layers, tokens, heads, hd, src, kv, page_rows, rope):
-    """Into "f8" pools; into "i8" pools the rows are read back too (a prompt's next piece attends over what the cache holds)."""
-    return {"name": name, "op": "append" if kv == "f8" else "store", "layers": layers, "tokens": tokens, "heads": heads, "hd": hd, "src": src, "kv": kv,
+    """Into "e4m3" pools; into "i8" pools the rows are read back too (a prompt's next piece attends over what the cache holds)."""
+    return {"name": name, "op": "append" if kv == "e4m3" else "store", "layers": layers, "tokens": tokens, "heads": heads, "hd": hd, "src": src, "kv": kv,
             "page_rows": page_rows, "rope": rope}
 
 
@@ -43,7 +43,7 @@ def _read(name, layers, tokens, heads, hd, to, kv, page_rows):
 
 
 def _fill(name, layers, dropped, B, heads, hd, page_rows):
-    return {"name": name, "op": "fill", "layers": layers, "dropped": dropped, "B": B, "heads": heads, "hd": hd, "kv": "f8", "page_rows": page_rows}
+    return {"name": name, "op": "fill", "layers": layers, "dropped": dropped, "B": B, "heads": heads, "hd": hd, "kv": "e4m3", "page_rows": page_rows}
 
 
 def _attend(name, B, rows, spread, heads, group, hd, act, kv, page_rows, new):
@@ -54,15 +54,15 @@ def _attend(name, B, rows, spread, heads, group, hd, act, kv, page_rows, new):
 def listed():
     return [
         # a prompt's keys and values of one block, rotated and quantised on their way into pages (7B widths)
-        _append("append_prompt_7b", 1, 512, 32, 128, "f32", "f8", 16, True),
+        _append("append_prompt_7b", 1, 512, 32, 128, "f32", "e4m3", 16, True),
         # the rows of a whole prompt pass moved into pages, several blocks in one call (70B widths, fp32 rows)
-        _append("append_blocks_70b", 8, 1024, 8, 128, "f32", "f8", 64, False),
+        _append("append_blocks_70b", 8, 1024, 8, 128, "f32", "e4m3", 64, False),
         # a piece of a prompt of odd length from a bf16 model, head_dim 64, and what the cache holds of it
         _append("store_piece_odd", 1, 77, 8, 64, "bf16", "i8", 16, True),
         # a long prompt of one block and what the cache holds of it (13B widths, fp16 rows)
         _append("store_prompt_13b", 1, 1024, 40, 128, "f16", "i8", 16, True),
         # a short sequence out of its pages, bf16, head_dim 64
-        _read("read_rows_odd", 1, 333, 8, 64, "bf16", "f8", 16),
+        _read("read_rows_odd", 1, 333, 8, 64, "bf16", "e4m3", 16),
         # a long sequence that leaves the pages: several blocks in one call (7B widths)
         _read("read_sequence_7b", 4, 2304, 32, 128, "f16", "i8", 32),
         # the blocks that a step dropped get the row of the last block that ran: one user
@@ -70,13 +70,13 @@ def listed():
         # the same of a batch and a deep model
         _fill("fill_70b_b8", 80, 40, 8, 8, 128, 64),
         # one user's step, nothing but latency (7B widths)
-        _attend("attend_7b_b1", 1, 640, "equal", 32, 1, 128, "f32", "f8", 16, True),
+        _attend("attend_7b_b1", 1, 640, "equal", 32, 1, 128, "f32", "e4m3", 16, True),
         # grouped queries (70B widths, batch 8), rows written before
         _attend("attend_70b_b8", 8, 1152, "equal", 8, 8, 128, "f32", "i8", 64, False),
         # requests of all ages, one to 32768 rows, some places empty; a bf16 model's queries, rows written before
         _attend("attend_ragged_b48", 48, 32768, "log", 8, 4, 128, "bf16", "i8", 16, False),
         # the full batch with long contexts: the largest stream of cache rows (7B widths, batch 32)
-        _attend("attend_7b_b32", 32, 2304, "equal", 32, 1, 128, "f32", "f8", 32, True),
+        _attend("attend_7b_b32", 32, 2304, "equal", 32, 1, 128, "f32", "e4m3", 32, True),
     ]
 
 
@@ -95,10 +95,10 @@ def _drawn(rng):
     op = rng.choice(["append", "read", "fill", "attend", "attend"])
     page_rows = rng.choice([16, 16, 32, 64, 128])
     hd = rng.choice([64, 128, 128])
-    kv = rng.choice(["i8", "f8"])
+    kv = rng.choice(["i8", "e4m3"])
     if op in ("append", "read"):
         heads, layers = rng.choice([1, 2, 4, 5, 8, 32, 40]), rng.choice([1, 1, 2, 5])
-        tokens = _between(rng, 1, min(6000, (1 << 26) // (heads * hd * layers)))
+        tokens = _between(rng, 1, min(6000, (1 << 25) // (heads * hd * layers)))
         kind = rng.choice(["f32", "bf16", "f16"])
         if op == "read":
             return _read("", layers, tokens, heads, hd, kind, kv, page_rows)
@@ -113,7 +113,7 @@ def _drawn(rng):
     heads = rng.choice([1, 2, 4, 8, 32] if group <= 4 else [1, 2, 8])
     most = max(16, min(32768, 540000000 // (B * heads * hd * 2 * max(1, group // 4))))
     return _attend("", B, _between(rng, 1, most), rng.choice(["equal", "log"]), heads, group, hd, rng.choice(["f32", "bf16", "f16"]), kv,
-                   page_rows, kv == "f8" and rng.random() < 0.7)
+                   page_rows, kv == "e4m3" and rng.random() < 0.7)
 
 
 def _lengths(case):
