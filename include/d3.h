@@ -38,7 +38,7 @@ typedef enum {
     D3_EDEVICE = -5  /* a HIP call failed */
 } d3_status;
 
-typedef enum { D3_F32 = 0, D3_BF16 = 1, D3_F16 = 2 } d3_dtype;
+typedef enum { D3_F32 = 0, D3_BF16 = 1, D3_F16 = 2, D3_I8 = 3, D3_E4M3 = 4 /* the last two: rows of a paged cache only */ } d3_dtype;
 typedef enum { D3_FILL_COPY = 0, D3_FILL_RECOMPUTE = 1 } d3_fill_mode;
 
 typedef struct {
@@ -235,8 +235,14 @@ int d3_truncate(d3_ctx *ctx, int32_t n_rows);
  *   slots       int32: where rows go, page * page_rows + row.
  * k_pages, v_pages: dev, a pool of n_pages pages per layer, of kv_dtype; every page holds page_rows rows of each KV head:
  *   K [layer][page][H_kv][page_rows][head_dim]
- *   V [layer][page][H_kv][page_rows / R][head_dim][R], R = 8 (D3_F16) or 4 (D3_F32) consecutive rows of one dim in 16 bytes,
- * as the matrix cores take them.  Values are clamped to +-65504 in D3_F16 pools; NaN stays.  A page number outside
+ *   V [layer][page][H_kv][page_rows / R][head_dim][R], R = 16 (D3_I8, D3_E4M3), 8 (D3_F16) or 4 (D3_F32) consecutive rows of one dim in 16 bytes,
+ * as the matrix cores take them.  Values are clamped to +-65504 in D3_F16 pools; NaN stays.
+ * Pools of 8 bits hold codes, whole numbers of 8 bits with a sign (D3_I8) or the e4m3 type (D3_E4M3: 4 bits of exponent, 3 of mantissa, largest 448, no infinities), and a scale for each row and head in
+ * k_scales, v_scales float [layer][page][H_kv][page_rows]: a row is code * scale.  As it is written (a key after it has turned, in fp32, every product and sum of the rotation rounded): with a its largest magnitude
+ * (3e38 at most, which an infinity counts as) and Q = 127 or 448, scale = a / Q, code = x * (Q / a) to nearest even; a < 2^-100: scale and codes are 0; a row with a NaN has the scale NaN.  A code is half a step
+ * off at most: a / 254 (D3_I8); 2^-4 |x|, or a 2^-10 / 448 near 0 (D3_E4M3).  What that does to logits grows with the blocks as d3_model_desc says of cache rows, from about 6.5e-3 (D3_I8) and 2.6e-2 (D3_E4M3) of a
+ * row's norm where its dims are alike: such caches are for callers who take that for half the bytes.  Where one dim is many times the others D3_I8 leaves those few codes, D3_E4M3 as many digits as before.
+ * A page number outside
  * [0, n_pages) in a table is a page that is not there: its rows count as masked.  A slot outside the pool is skipped.
  * A row may be given to one slot at a time (two rows of one call with the same slot: either is kept, element by element).
  * Calls on one d3_pages must be ordered (one stream, or streams that wait for each other; replays of graphs too): they share
@@ -244,7 +250,7 @@ int d3_truncate(d3_ctx *ctx, int32_t n_rows);
  * be used at the same time as far as neither writes what the other reads. */
 typedef struct {
     int32_t n_layers, n_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128; n_heads % n_kv_heads == 0 */
-    int32_t kv_dtype;                                  /* D3_F16 or D3_F32, see d3_model_desc */
+    int32_t kv_dtype;                                  /* D3_F16 or D3_F32, see d3_model_desc; D3_I8, D3_E4M3 */
     int32_t n_pages, page_rows;                        /* page_rows: a power of two in [16, 1024]; n_pages * page_rows < 2^31 */
     int32_t max_batch, max_pages;                      /* sequences (at most 4096); pages of one (max_pages * page_rows <= 2^30); max_batch * max_pages < 2^31 */
 } d3_pages_desc;
@@ -259,6 +265,9 @@ size_t d3_pages_workspace_size(const d3_pages_desc *desc);
  * memory, and no stream may be capturing. */
 int d3_pages_create(d3_pages **out, const d3_pages_desc *desc, void *k_pages, void *v_pages, void *workspace, size_t workspace_bytes);
 int d3_pages_destroy(d3_pages *pages);
+
+/* d3_pages_create of pools of 8 bits (D3_I8, D3_E4M3), which it refuses: k_scales, v_scales dev, 16-byte aligned, the caller's as the pools are.  Every call below takes either handle. */
+int d3_pages_create_scaled(d3_pages **out, const d3_pages_desc *desc, void *k_pages, void *v_pages, float *k_scales, float *v_scales, void *workspace, size_t workspace_bytes);
 
 /* Page tables and slot maps from request lengths.  Granted pages are not cleared: they hold what their last owner left.  added: dev int32 [B]: how many rows sequence b asks for (0: none; negative: the sequence has
  * ended, its pages go back and its rows become 0).  Pages of ended sequences are pushed first, in the order of b and of their tables.  Then the
@@ -280,6 +289,11 @@ int d3_pages_reserve(d3_pages *pages, int32_t B, const int32_t *added, const int
 int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t *slots, const void *k, const void *v, int32_t dtype,
                     int64_t token_stride, int64_t head_stride, int64_t layer_stride, const float *rope_cs, void *hip_stream);
 
+/* The other way round: rows `slots` of `n_layers` layers from `layer` on, as the pools hold them (keys as they were turned), into k, v: dev [n_layers][n][H_kv][head_dim] of `dtype` (D3_F32, D3_BF16 or D3_F16), by
+ * the strides of d3_pages_append.  From pools of 8 bits code * scale is rounded to fp32, then to `dtype`; from the others the value once.  Rows of slots outside the pool are left as they are; a slot may be listed
+ * more than once.  n at most 2^28. */
+int d3_pages_read(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t *slots, void *k, void *v, int32_t dtype, int64_t token_stride, int64_t head_stride, int64_t layer_stride, void *hip_stream);
+
 /* The rows of the sequences that a reserve gave some, 0 for the others (refused, paused, ended): live[b] = starts[b] == starts[b + 1] ? 0 : rows[b], b < B, all dev int32, starts as
  * d3_pages_reserve wrote it.  As `rows` of d3_pages_attention it leaves the others out: nothing of them is read or written but their out, which is 0. */
 int d3_pages_live(d3_pages *pages, int32_t B, const int32_t *rows, const int32_t *starts, int32_t *live, void *hip_stream);
@@ -290,12 +304,12 @@ int d3_pages_live(d3_pages *pages, int32_t B, const int32_t *rows, const int32_t
  * The call cannot tell a sequence that a reserve refused, or that asked for nothing: it would lose its newest row, so `rows` is then d3_pages_live's.  rope_cs: dev float [B][head_dim / 2][2]: q and
  * k_new turn by it; NULL: neither does.  q, k_new, v_new, rope_cs 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
  * out may be q itself.  Keys and values are used as the pool holds them; sums, maxima and partial results are in 32 bits.  Into the products q and the weights go in fp32 with D3_F32 pools, as
- * the sum of two fp16 halves (22 bits) with D3_F16 pools.  A row whose score is -infinity has the weight 0; out is 0 too where every row's is. */
+ * the sum of two fp16 halves (22 bits) with D3_F16 pools and those of 8 bits, where a weight is multiplied by its row's scale first; the halves of these products count in steps of 2^-40 of the largest so far.  A row whose score is -infinity has the weight 0; out is 0 too where every row's is. */
 int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,
                        int64_t kv_stride, const float *rope_cs, const int32_t *tables, const int32_t *rows, float scale, void *out,
                        int64_t out_stride, void *hip_stream);
 
-/* The missing-state fill on pages (D3_FILL_COPY, Section 3.2): rows `slots` of layer `src` are copied into layers [first, first + n_layers), which
+/* The missing-state fill on pages (D3_FILL_COPY, Section 3.2): rows `slots` of layer `src` are copied (codes and scales of pools of 8 bits, nothing is rounded again) into layers [first, first + n_layers), which
  * must not hold src; src < 0: zeros.  n * H_kv at most 2^25. */
 int d3_pages_fill(d3_pages *pages, int32_t n, const int32_t *slots, int32_t src, int32_t first, int32_t n_layers, void *hip_stream);
 
@@ -309,7 +323,7 @@ int d3_store_pages(d3_ctx *ctx, d3_pages *pages, int32_t seq, int32_t row_begin,
  * plan, 0 <= step_i < n_steps, in any order of steps; the context's own cache, row count and step counter stay as they are.  A block that the step drops gets no row: until
  * d3_fill_missing_paged has filled it, the pages hold there what they held before, another request's row if they are another's former pages.  So a step is followed by the fill of its
  * slots before any step that runs a block it dropped; only where every later step of these sequences drops these blocks too (a request's own steps in order, by a shrinking depth) it may be left out.
- * D3_ESHAPE unless the pages have the context's shape and cache type;
+ * D3_ESHAPE unless the pages have the context's shape, and its cache type or one of 8 bits;
  * D3_ESTATE with D3_FILL_RECOMPUTE. */
 int d3_decode_step_paged(d3_ctx *ctx, d3_pages *pages, const int32_t *tok_in, int32_t B, int32_t step_i, const int32_t *tables,
                          const int32_t *rows, int32_t *tok_out, float *logits, float *hidden_dump, void *hip_stream);

@@ -13,7 +13,7 @@ import numpy as np
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB: Optional[C.CDLL] = None
 
-D3_F32, D3_BF16, D3_F16 = 0, 1, 2
+D3_F32, D3_BF16, D3_F16, D3_I8, D3_E4M3 = 0, 1, 2, 3, 4
 D3_FILL_COPY = 0
 D3_FILL_RECOMPUTE = 1
 D3_K_NONE, D3_K_QKV, D3_K_ATTN, D3_K_OPROJ, D3_K_GATE_UP, D3_K_DOWN, D3_K_LM_HEAD, D3_K_EMPTY = range(8)
@@ -84,9 +84,11 @@ def load_library() -> C.CDLL:
         lib.d3_pages_workspace_size.argtypes = [C.POINTER(_PagesDesc)]
         lib.d3_pages_workspace_size.restype = C.c_size_t
         lib.d3_pages_create.argtypes = [C.POINTER(vp), C.POINTER(_PagesDesc), vp, vp, vp, C.c_size_t]
+        lib.d3_pages_create_scaled.argtypes = [C.POINTER(vp), C.POINTER(_PagesDesc), vp, vp, vp, vp, vp, C.c_size_t]
         lib.d3_pages_destroy.argtypes = [vp]
         lib.d3_pages_reserve.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
         lib.d3_pages_append.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, i64, i64, i64, vp, vp]
+        lib.d3_pages_read.argtypes = [vp, i32, i32, i32, vp, vp, vp, i32, i64, i64, i64, vp]
         lib.d3_pages_attention.argtypes = [vp, i32, i32, vp, vp, vp, i32, i64, i64, vp, vp, vp, C.c_float, vp, i64, vp]
         lib.d3_pages_live.argtypes = [vp, i32, vp, vp, vp, vp]
         lib.d3_pages_fill.argtypes = [vp, i32, vp, i32, i32, i32, vp]
@@ -318,12 +320,13 @@ class PagedCache:
     streams have used goes away, these have to be waited for.
 
     k_pages [n_layers][n_pages][n_kv_heads][page_rows][head_dim] and v_pages [n_layers][n_pages][n_kv_heads][page_rows / R][head_dim][R]
-    (R = 8 for "f16", 4 for "f32"); tables int32 [max_batch][max_pages]; rows int32 [max_batch]; free_pages int32 [n_pages], a stack of which
+    (R = 16 for "i8" and "e4m3", 8 for "f16", 4 for "f32"); with "i8" and "e4m3" k_scales and v_scales float32 [n_layers][n_pages][n_kv_heads][page_rows], by which a row's codes are
+    multiplied (None with the others); tables int32 [max_batch][max_pages]; rows int32 [max_batch]; free_pages int32 [n_pages], a stack of which
     the first n_free[0] entries count.  Buffers that are not given are made: pools of zeros, no sequences, all pages free."""
 
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, n_pages: int, page_rows: int, max_batch: int, max_pages: int,
                  kv_dtype: str = "f16", n_layers: int = 1, k_pages=None, v_pages=None, tables=None, rows=None, free_pages=None, n_free=None,
-                 device: str = "cuda:0"):
+                 device: str = "cuda:0", k_scales=None, v_scales=None):
         import torch
         self.torch = torch
         self.lib = load_library()
@@ -333,7 +336,7 @@ class PagedCache:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.n_layers, self.n_heads, self.n_kv_heads, self.head_dim = n_layers, n_heads, n_kv_heads, head_dim
         self.n_pages, self.page_rows, self.max_batch, self.max_pages, self.kv_dtype = n_pages, page_rows, max_batch, max_pages, kv_dtype
-        kinds = {"f32": D3_F32, "bf16": D3_BF16, "f16": D3_F16}
+        kinds = {"f32": D3_F32, "bf16": D3_BF16, "f16": D3_F16, "i8": D3_I8, "e4m3": D3_E4M3}
         if kv_dtype not in kinds:
             raise ValueError(f"kv_dtype must be one of {sorted(kinds)} (got {kv_dtype!r})")
         desc = _PagesDesc(n_layers, n_heads, n_kv_heads, head_dim, kinds[kv_dtype], n_pages, page_rows, max_batch, max_pages)
@@ -345,7 +348,7 @@ class PagedCache:
         self._index = self.device.index
         # the current stream's handle without the object around it (2 us a call), where torch offers that
         self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
-        tdt = {"f32": torch.float32, "f16": torch.float16}[kv_dtype]
+        tdt = {"f32": torch.float32, "f16": torch.float16, "i8": torch.int8, "e4m3": torch.float8_e4m3fn}[kv_dtype]
         unit = 16 // tdt.itemsize
         with torch.cuda.device(self.device):
             def buffer(name, given, dims, dtype, make):
@@ -356,6 +359,12 @@ class PagedCache:
                 return given
             self.k_pages = buffer("k_pages", k_pages, (n_layers, n_pages, n_kv_heads, page_rows, head_dim), tdt, torch.zeros)
             self.v_pages = buffer("v_pages", v_pages, (n_layers, n_pages, n_kv_heads, page_rows // unit, head_dim, unit), tdt, torch.zeros)
+            self.k_scales = self.v_scales = None
+            if unit == 16:
+                self.k_scales = buffer("k_scales", k_scales, (n_layers, n_pages, n_kv_heads, page_rows), torch.float32, torch.zeros)
+                self.v_scales = buffer("v_scales", v_scales, (n_layers, n_pages, n_kv_heads, page_rows), torch.float32, torch.zeros)
+            elif k_scales is not None or v_scales is not None:
+                raise ValueError(f"k_scales and v_scales belong to kv_dtype 'i8' and 'e4m3' (got {kv_dtype!r})")
             none = lambda dims, **kw: torch.full(dims, -1, **kw)
             self.tables = buffer("tables", tables, (max_batch, max_pages), torch.int32, none)
             self.rows = buffer("rows", rows, (max_batch,), torch.int32, torch.zeros)
@@ -368,8 +377,11 @@ class PagedCache:
             # The counters are cleared on the null stream, which does not wait for this one, where work on memory that the workspace was made from may still be queued.
             torch.cuda.current_stream(self.device).synchronize()
             handle = C.c_void_p()
-            _check(self.lib.d3_pages_create(C.byref(handle), C.byref(desc), self.k_pages.data_ptr(), self.v_pages.data_ptr(),
-                                            self.workspace.data_ptr(), ws_bytes))
+            pools = (self.k_pages.data_ptr(), self.v_pages.data_ptr())
+            if unit == 16:
+                _check(self.lib.d3_pages_create_scaled(C.byref(handle), C.byref(desc), *pools, self.k_scales.data_ptr(), self.v_scales.data_ptr(), self.workspace.data_ptr(), ws_bytes))
+            else:
+                _check(self.lib.d3_pages_create(C.byref(handle), C.byref(desc), *pools, self.workspace.data_ptr(), ws_bytes))
         self.handle = handle
 
     def close(self) -> None:
@@ -409,6 +421,17 @@ class PagedCache:
             raise ValueError(f"{name} must be a {dtype} tensor {tuple(dims)} on {self.device}, its last dim dense{'' if strides is None else f', with strides {strides}'}")
         return own
 
+    def _rows(self, slots, k, v):
+        """(layers, rows, type, strides of row, head and layer) of k and v for append and read."""
+        self._ints(slots=slots)
+        n, kind = slots.numel(), self._kind(k)
+        layers = k.shape[0] if k.dim() == 4 else 1
+        dims = (layers, n, self.n_kv_heads, self.head_dim) if k.dim() == 4 else (n, self.n_kv_heads, self.head_dim)
+        strides = self._heads("k", k, dims, k.dtype)
+        self._heads("v", v, dims, k.dtype, strides)
+        # (the stride of a dim with one entry says nothing)
+        return layers, n, kind, (strides[-3] if n > 1 else 0, strides[-2] if self.n_kv_heads > 1 else 0, strides[0] if layers > 1 else 0)
+
     def _kind(self, t) -> int:
         kind = self._kinds.get(t.dtype)
         if kind is None:
@@ -440,15 +463,23 @@ class PagedCache:
         """k, v [n][n_kv_heads][head_dim], or [m][n][n_kv_heads][head_dim] for the m layers from `layer` on, into the rows `slots` (int32 CUDA tensor [n]) of the pools.  k and v have
         the same strides, the last dim dense.
         rope_cs [n][head_dim / 2][2]: (cos, sin) by which the keys turn first."""
-        self._ints(slots=slots)
-        n, kind = slots.numel(), self._kind(k)
-        layers = k.shape[0] if k.dim() == 4 else 1
-        dims = (layers, n, self.n_kv_heads, self.head_dim) if k.dim() == 4 else (n, self.n_kv_heads, self.head_dim)
-        strides = self._heads("k", k, dims, k.dtype)
-        self._heads("v", v, dims, k.dtype, strides)
-        # (the stride of a dim with one entry says nothing)
-        _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, strides[-3] if n > 1 else 0,
-                                        strides[-2] if self.n_kv_heads > 1 else 0, strides[0] if layers > 1 else 0, self._angles(rope_cs, n), self._stream()))
+        layers, n, kind, strides = self._rows(slots, k, v)
+        _check(self.lib.d3_pages_append(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, *strides, self._angles(rope_cs, n), self._stream()))
+
+    def read(self, layer: int, slots, k=None, v=None, dtype=None, n_layers: Optional[int] = None):
+        """The rows `slots` (int32 CUDA tensor [n]) as the pools hold them, keys as they were turned: into k, v [n][n_kv_heads][head_dim], or [m][n][n_kv_heads][head_dim] of the m layers from
+        `layer` on, which have the same strides, the last dim dense, and are returned.  Rows of slots outside the pools are left as they are.  Where k and v are left out they are made, of `dtype`
+        (float32 if that is left out too), for n_layers layers, or without that dim for one; rows of slots outside the pools are then 0."""
+        if k is None and v is None:
+            dims = (slots.numel(), self.n_kv_heads, self.head_dim) if n_layers is None else (n_layers, slots.numel(), self.n_kv_heads, self.head_dim)
+            k, v = (self.torch.zeros(dims, dtype=dtype or self._float32, device=self.device) for _ in range(2))
+        elif k is None or v is None:
+            raise ValueError("k and v come together or not at all")
+        elif dtype is not None or n_layers is not None:
+            raise ValueError("dtype and n_layers are for k and v that are left out")
+        layers, n, kind, strides = self._rows(slots, k, v)
+        _check(self.lib.d3_pages_read(self.handle, layer, layers, n, slots.data_ptr(), k.data_ptr(), v.data_ptr(), kind, *strides, self._stream()))
+        return k, v
 
     def attend(self, layer: int, q, k=None, v=None, rope_cs=None, scale: float = 0.0, out=None, starts=None):
         """Attention of one token of each of the first B sequences, q [B][n_heads][head_dim], over their rows; returns out [B][n_heads][head_dim] of q's dtype.

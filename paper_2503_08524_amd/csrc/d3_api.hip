@@ -587,7 +587,7 @@ int forward(d3_ctx* c, const int32_t* tokens, ColMap cm, int ncols, const int32_
             pa.rope_cs = rope_cs; pa.tables = paged->tables; pa.rows = paged_rows;
             pa.out = at.out; pa.out_split = at.out_split; pa.out_form = at.out_form;
             Timed t(c, D3_K_ATTN, s);
-            D3_HIP(launch_attention_paged(pa, hd, d.kv_dtype, c->n_cu, s));
+            D3_HIP(launch_attention_paged(pa, hd, paged->pages->desc.kv_dtype, c->n_cu, s));
         } else if (shared && !prompt_attn) {
             for (int r = 0; r < runs.n; ++r) {         // one after the other: the partials and the counters are the launch's own
                 const int col = runs.col[r];
@@ -936,11 +936,11 @@ extern "C" int d3_decode_step_static(d3_ctx* ctx, const int32_t* tok_in, int32_t
 
 namespace {
 
-// The pages' rows are of the context's shape and on its GPU; for a step, its query heads and its cache's type too.
+// The pages' rows are of the context's shape and on its GPU; for a step, its query heads and its cache's type (or one of 8 bits) too.
 int check_pages(const d3_ctx* ctx, const d3_pages* pages, const char* who, bool step) {
     const d3_model_desc& d = ctx->desc;
     const d3_pages_desc& p = pages->desc;
-    if (p.n_layers != d.n_layers || p.n_kv_heads != d.n_kv_heads || p.head_dim != d.head_dim || (step && (p.n_heads != d.n_heads || p.kv_dtype != d.kv_dtype)))
+    if (p.n_layers != d.n_layers || p.n_kv_heads != d.n_kv_heads || p.head_dim != d.head_dim || (step && (p.n_heads != d.n_heads || (p.kv_dtype != d.kv_dtype && !pages->scaled()))))
         return fail(D3_ESHAPE, "%s: the pages' layers, %s, head_dim%s must be the context's", who, step ? "heads" : "KV heads", step ? " and type" : "");
     if (pages->dev != ctx->dev) return fail(D3_EINVAL, "%s: the pages are on device %d, the context on %d", who, pages->dev, ctx->dev);
     return D3_OK;

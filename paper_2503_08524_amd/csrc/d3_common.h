@@ -25,8 +25,8 @@ constexpr int kSsqStride = 512;    // partial sums of squares kept per column (o
 typedef uint16_t bf16_t;           // bf16 bit pattern
 typedef _Float16 f16_t;            // IEEE half (KV cache only)
 
-// bytes per KV-cache element for a d3_dtype value (0 f32, 2 f16)
-inline int kv_elem_bytes(int kv_dtype) { return kv_dtype == 0 ? 4 : 2; }
+// bytes per KV-cache element for a d3_dtype value (0 f32, 2 f16; of paged caches 3 i8, 4 e4m3)
+inline int kv_elem_bytes(int kv_dtype) { return kv_dtype == 0 ? 4 : kv_dtype >= 3 ? 1 : 2; }
 
 // Division by a number that the host knows: a multiplication and a correction instead of the 25 dependent instructions of a division.  With
 // m = floor(2^32 / d) (one less for d = 1) the product's upper word is the quotient or one less, for every x in [0, 2^31).

@@ -26,7 +26,7 @@ int check_desc(const d3_pages_desc* d) {
     if (d->n_heads % d->n_kv_heads != 0) return fail(D3_ESHAPE, "pages: n_heads (%d) must be a multiple of n_kv_heads (%d)", d->n_heads, d->n_kv_heads);
     if (d->head_dim != 64 && d->head_dim != 128) return fail(D3_ESHAPE, "pages: head_dim must be 64 or 128 (got %d)", d->head_dim);
     if (d->kv_dtype == D3_BF16) return fail(D3_EINVAL, "pages: kv_dtype D3_BF16 is not offered (an 8-bit mantissa, see d3_model_desc); use D3_F16 (same bytes) or D3_F32");
-    if (d->kv_dtype != D3_F32 && d->kv_dtype != D3_F16) return fail(D3_EINVAL, "pages: kv_dtype must be D3_F32 or D3_F16");
+    if (d->kv_dtype != D3_F32 && d->kv_dtype != D3_F16 && d->kv_dtype != D3_I8 && d->kv_dtype != D3_E4M3) return fail(D3_EINVAL, "pages: kv_dtype must be D3_F32, D3_F16, D3_I8 or D3_E4M3 (got %d)", d->kv_dtype);
     if (d->page_rows < 16 || d->page_rows > 1024 || (d->page_rows & (d->page_rows - 1)) != 0) return fail(D3_ESHAPE, "pages: page_rows must be a power of two in [16, 1024] (got %d)", d->page_rows);
     if (d->n_pages < 1 || (int64_t)d->n_pages * d->page_rows > INT32_MAX) return fail(D3_ESHAPE, "pages: n_pages must be positive and n_pages * page_rows below 2^31 (got %d, %d)", d->n_pages, d->page_rows);
     if (d->max_batch < 1 || d->max_batch > kPagesMaxSeqs) return fail(D3_ESHAPE, "pages: max_batch must be in [1, %d] (got %d)", kPagesMaxSeqs, d->max_batch);
@@ -102,10 +102,8 @@ extern "C" size_t d3_pages_workspace_size(const d3_pages_desc* desc) {
     return layout(*desc, &ml, &tickets);
 }
 
-extern "C" int d3_pages_create(d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pages, void* workspace, size_t workspace_bytes) {
-    if (!out) return fail(D3_EINVAL, "d3_pages_create: out is NULL");
-    *out = nullptr;
-    D3_CHECK(check_desc(desc));
+namespace {
+int create(d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pages, float* k_scales, float* v_scales, void* workspace, size_t workspace_bytes) {
     if (!k_pages || !v_pages || !workspace) return fail(D3_EINVAL, "d3_pages_create: pool or workspace is NULL");
     if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(D3_EINVAL, "d3_pages_create: the pools must be 16-byte aligned");
     if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(D3_EINVAL, "d3_pages_create: workspace must be %zu-byte aligned", kAlign);
@@ -119,6 +117,7 @@ extern "C" int d3_pages_create(d3_pages** out, const d3_pages_desc* desc, void* 
     if (!p) return fail(D3_EINVAL, "d3_pages_create: out of host memory");
     p->desc = *desc;
     p->k = static_cast<char*>(k_pages); p->v = static_cast<char*>(v_pages); p->ws = static_cast<char*>(workspace);
+    p->ks = k_scales; p->vs = v_scales;
     p->dev = dev; p->n_cu = n_cu;
     p->part_ml = part_ml; p->tickets = tickets;
     hipError_t e = hipMemset(p->ws + tickets, 0, need - tickets);              // arrival counters start at 0
@@ -126,6 +125,25 @@ extern "C" int d3_pages_create(d3_pages** out, const d3_pages_desc* desc, void* 
     if (e != hipSuccess) { delete p; return fail(D3_EDEVICE, "d3_pages_create: hipMemset failed: %s", hipGetErrorString(e)); }
     *out = p;
     return D3_OK;
+}
+}  // namespace
+
+extern "C" int d3_pages_create(d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pages, void* workspace, size_t workspace_bytes) {
+    if (!out) return fail(D3_EINVAL, "d3_pages_create: out is NULL");
+    *out = nullptr;
+    D3_CHECK(check_desc(desc));
+    if (kv_elem_bytes(desc->kv_dtype) == 1) return fail(D3_EINVAL, "d3_pages_create: pools of 8 bits have scales (d3_pages_create_scaled)");
+    return create(out, desc, k_pages, v_pages, nullptr, nullptr, workspace, workspace_bytes);
+}
+
+extern "C" int d3_pages_create_scaled(d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pages, float* k_scales, float* v_scales, void* workspace, size_t workspace_bytes) {
+    if (!out) return fail(D3_EINVAL, "d3_pages_create_scaled: out is NULL");
+    *out = nullptr;
+    D3_CHECK(check_desc(desc));
+    if (kv_elem_bytes(desc->kv_dtype) != 1) return fail(D3_EINVAL, "d3_pages_create_scaled: only pools of 8 bits (D3_I8, D3_E4M3) have scales (d3_pages_create)");
+    if (!k_scales || !v_scales) return fail(D3_EINVAL, "d3_pages_create_scaled: scales are NULL");
+    if (!aligned16(k_scales) || !aligned16(v_scales)) return fail(D3_EINVAL, "d3_pages_create_scaled: the scales must be 16-byte aligned");
+    return create(out, desc, k_pages, v_pages, k_scales, v_scales, workspace, workspace_bytes);
 }
 
 extern "C" int d3_pages_destroy(d3_pages* pages) {
@@ -179,8 +197,34 @@ extern "C" int d3_pages_append(d3_pages* pages, int32_t layer, int32_t n_layers,
     a.rope_cs = reinterpret_cast<const float2*>(rope_cs);
     a.pool_bytes = pages->pool_bytes();
     a.k_pages = pages->k + layer * a.pool_bytes; a.v_pages = pages->v + layer * a.pool_bytes;
+    a.k_scales = pages->ks + layer * pages->layer_scales(); a.v_scales = pages->vs + layer * pages->layer_scales(); a.scale_bytes = pages->layer_scales() * 4;
     const OnDevice on(pages->dev);
     D3_HIP(launch_pages_append(a, d.kv_dtype, static_cast<hipStream_t>(hip_stream)));
+    return D3_OK;
+}
+
+extern "C" int d3_pages_read(d3_pages* pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t* slots, void* k, void* v, int32_t dtype, int64_t token_stride, int64_t head_stride,
+                             int64_t layer_stride, void* hip_stream) {
+    if (!pages) return fail(D3_EINVAL, "d3_pages_read: pages is NULL");
+    D3_CHECK(check_tokens("d3_pages_read", n));
+    D3_CHECK(check_layers(pages, "d3_pages_read", layer, n_layers));
+    D3_CHECK(check_dtype("d3_pages_read", dtype));
+    if (n > kMostAppendTokens) return fail(D3_ESHAPE, "d3_pages_read: %d rows are more than one launch counts (%d)", n, kMostAppendTokens);
+    if (n == 0) return D3_OK;
+    if (!slots || !k || !v) return fail(D3_EINVAL, "d3_pages_read: NULL argument");
+    const int unit = 16 / elem_bytes(dtype);
+    if (!aligned16(k) || !aligned16(v) || token_stride % unit != 0 || head_stride % unit != 0 || layer_stride % unit != 0)
+        return fail(D3_EINVAL, "d3_pages_read: k, v and their strides must be multiples of 16 bytes");
+    const d3_pages_desc& d = pages->desc;
+    ReadArgs a{};
+    a.n = n; a.n_layers = n_layers; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_shift = __builtin_ctz(d.page_rows); a.n_slots = pages->n_slots();
+    a.slots = slots; a.k = k; a.v = v; a.dtype = dtype;
+    a.token_stride = token_stride; a.head_stride = head_stride; a.layer_stride = layer_stride;
+    a.pool_bytes = pages->pool_bytes(); a.scale_bytes = pages->layer_scales() * 4;
+    a.k_pages = pages->k + layer * a.pool_bytes; a.v_pages = pages->v + layer * a.pool_bytes;
+    a.k_scales = pages->ks + layer * pages->layer_scales(); a.v_scales = pages->vs + layer * pages->layer_scales();
+    const OnDevice on(pages->dev);
+    D3_HIP(launch_pages_read(a, d.kv_dtype, static_cast<hipStream_t>(hip_stream)));
     return D3_OK;
 }
 
@@ -222,6 +266,7 @@ extern "C" int d3_pages_fill(d3_pages* pages, int32_t n, const int32_t* slots, i
     a.n = n; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_shift = __builtin_ctz(d.page_rows); a.by_heads = Divisor(d.n_kv_heads); a.first = first; a.n_layers = n_layers; a.src = src < 0 ? -1 : src;
     a.n_slots = pages->n_slots();
     a.slots = slots; a.k_pages = pages->k; a.v_pages = pages->v; a.pool_bytes = pages->pool_bytes();
+    a.k_scales = pages->ks; a.v_scales = pages->vs; a.scale_bytes = pages->layer_scales() * 4;
     const OnDevice on(pages->dev);
     D3_HIP(launch_pages_fill(a, d.kv_dtype, static_cast<hipStream_t>(hip_stream)));
     return D3_OK;

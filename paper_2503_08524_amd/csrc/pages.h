@@ -1,7 +1,7 @@
 // The paged key-value cache: handle, kernel arguments and launch wrappers.
 //
 // A page holds page_rows rows of every KV head.  Keys are [page][head][row][dim]; values [page][head][row / R][dim][row % R] with
-// R = 16 bytes / element (8 fp16, 4 fp32): R consecutive rows of one dim are the 16 bytes that a lane of the matrix cores wants of V
+// R = 16 bytes / element (16 of 8 bits, 8 fp16, 4 fp32): R consecutive rows of one dim are the 16 bytes that a lane of the matrix cores wants of V
 // when it weighs rows, as 16 bytes of a row are what it wants of K, so both go from memory to the matrix cores without passing through LDS.
 #pragma once
 #include "d3_common.h"
@@ -44,8 +44,25 @@ struct AppendArgs {
     const float2* rope_cs;                 // optional [n][hd / 2]
     void *k_pages, *v_pages;               // the first layer's pools
     size_t pool_bytes;                     // of a layer
+    float *k_scales, *v_scales;            // 8-bit pools: the first layer's scales, [page][H_kv][page_rows]
+    size_t scale_bytes;                    // of a layer
 };
 int launch_pages_append(const AppendArgs& a, int kv_dtype, hipStream_t s);
+int launch_pages_append8(const AppendArgs& a, int kv_dtype, hipStream_t s);     // D3_I8, D3_E4M3
+
+struct ReadArgs {                          // as AppendArgs, the other way round
+    int n, n_layers, H_kv, hd, page_shift;
+    long long n_slots;
+    const int32_t* slots;
+    void *k, *v;
+    int dtype;
+    long long token_stride, head_stride, layer_stride;
+    const void *k_pages, *v_pages;
+    size_t pool_bytes;
+    const float *k_scales, *v_scales;
+    size_t scale_bytes;
+};
+int launch_pages_read(const ReadArgs& a, int kv_dtype, hipStream_t s);
 
 struct PagesFillArgs {
     int n, H_kv, hd, page_shift, first, n_layers, src;     // src < 0: zeros
@@ -54,6 +71,8 @@ struct PagesFillArgs {
     const int32_t* slots;
     void *k_pages, *v_pages;               // layer 0
     size_t pool_bytes;
+    float *k_scales, *v_scales;            // 8-bit pools, layer 0
+    size_t scale_bytes;
 };
 int launch_pages_fill(const PagesFillArgs& a, int kv_dtype, hipStream_t s);
 
@@ -67,6 +86,7 @@ struct PagedAttnArgs {
     int B, H_kv, group, n_pages, page_shift;
     float scale;                           // of the scores
     void *k_pages, *v_pages;               // this layer's pools
+    float *k_scales, *v_scales;            // ... and, of 8-bit rows, their scales
     void* out;
     bf16_t* out_split;                     // optional split copy
     SplitForm out_form;
@@ -75,6 +95,7 @@ struct PagedAttnArgs {
     Divisor by_runs, by_waves;             // set by launch_attention_paged: its workgroups and their waves
 };
 int launch_attention_paged(const PagedAttnArgs& a, int hd, int kv_dtype, int n_cu, hipStream_t s);
+int launch_attention_paged8(const PagedAttnArgs& a, int hd, int kv_dtype, int n_cu, hipStream_t s);    // D3_I8, D3_E4M3
 // rows of a wave's turn: 16 loads of 16 bytes a lane
 inline int paged_turn_rows(int hd, int kv_dtype) { return 16 * 64 * 16 / (2 * hd * kv_elem_bytes(kv_dtype)); }
 inline int paged_head_tiles(int group) { return (group + kPagedHeads - 1) / kPagedHeads; }
@@ -84,11 +105,14 @@ inline int paged_head_tiles(int group) { return (group + kPagedHeads - 1) / kPag
 struct d3_pages {
     d3_pages_desc desc;
     char *k, *v, *ws;
+    float *ks, *vs;                        // scales of 8-bit pools
     int dev, n_cu;
     size_t part_ml, tickets;               // byte offsets into the workspace; the partial outputs are first
     size_t pool_bytes() const {
         return (size_t)desc.n_pages * desc.n_kv_heads * desc.page_rows * desc.head_dim * d3::kv_elem_bytes(desc.kv_dtype);
     }
+    bool scaled() const { return d3::kv_elem_bytes(desc.kv_dtype) == 1; }
+    size_t layer_scales() const { return scaled() ? (size_t)desc.n_pages * desc.n_kv_heads * desc.page_rows : 0; }
     long long n_slots() const { return (long long)desc.n_pages * desc.page_rows; }
 };
 
@@ -102,6 +126,7 @@ inline PagedAttnArgs paged_attn_args(const d3_pages* p, int layer, int B) {
     a.n_pages = d.n_pages; a.page_shift = __builtin_ctz(d.page_rows);
     a.table_stride = d.max_pages; a.max_rows = d.max_pages * d.page_rows;
     a.k_pages = p->k + (size_t)layer * p->pool_bytes(); a.v_pages = p->v + (size_t)layer * p->pool_bytes();
+    a.k_scales = p->ks + layer * p->layer_scales(); a.v_scales = p->vs + layer * p->layer_scales();
     a.part_o = reinterpret_cast<float*>(p->ws); a.part_ml = reinterpret_cast<float*>(p->ws + p->part_ml);
     a.tickets = reinterpret_cast<int*>(p->ws + p->tickets);
     return a;

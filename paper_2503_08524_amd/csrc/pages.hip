@@ -338,6 +338,13 @@ __global__ __launch_bounds__(256) void pages_fill_kernel(PagesFillArgs a, int la
 #pragma unroll
         for (int d = 0; d < DL; ++d) vv[d] = *reinterpret_cast<const T*>(v_at + a.src * a.pool_bytes + d * 16);
     }
+    if constexpr (sizeof(T) == 1) {                                 // the row's scales: of the key in lane 0, of the value in lane 1
+        if (lane < 2) {
+            char* s_at = reinterpret_cast<char*>((lane == 0 ? a.k_scales : a.v_scales) + base / HD + row);
+            const float scale = a.src >= 0 ? *reinterpret_cast<const float*>(s_at + a.src * a.scale_bytes) : 0.f;
+            for (int l = l0; l < l1; ++l) *reinterpret_cast<float*>(s_at + l * a.scale_bytes) = scale;
+        }
+    }
     for (int l = l0; l < l1; ++l) {
         if (has_key) *reinterpret_cast<uint4*>(k_at + l * a.pool_bytes) = kv;
 #pragma unroll
@@ -394,10 +401,12 @@ int launch_pages_live(const int32_t* rows, const int32_t* starts, int max_rows, 
 }
 
 int launch_pages_append(const AppendArgs& a, int kv_dtype, hipStream_t s) {
+    if (kv_elem_bytes(kv_dtype) == 1) return launch_pages_append8(a, kv_dtype, s);
     return kv_dtype == D3_F32 ? launch_append_to<float>(a, s) : launch_append_to<f16_t>(a, s);
 }
 
 int launch_pages_fill(const PagesFillArgs& a, int kv_dtype, hipStream_t s) {
+    if (kv_elem_bytes(kv_dtype) == 1) return launch_fill<uint8_t>(a, s);
     return kv_dtype == D3_F32 ? launch_fill<float>(a, s) : launch_fill<f16_t>(a, s);
 }
 
