@@ -174,9 +174,9 @@ struct Runs {
     int per, more;
     __device__ Runs(int total, const Divisor& by) : per(by.of(total)), more(total - per * by.d) {}
     __device__ int begin(int w) const { return w * per + min(w, more); }
-    __device__ int of(int x) const {                               // the run that unit x is in
-        const int larger = more * (per + 1);
-        return x < larger ? small_quotient(x, per + 1) : more + small_quotient(x - larger, max(per, 1));      // per = 0: every unit is below `larger`
+    __device__ int of(int x, int none = 0) const {                 // the run that unit x is in; none: 0, which the compiler need not know
+        const int larger = more * (per + 1), each = per + none;
+        return x < larger ? small_quotient(x, each + 1) : more + small_quotient(x - larger, max(each, 1));    // per = 0: every unit is below `larger`
     }
 };
 
@@ -223,7 +223,7 @@ template <typename T, int HD, typename A, bool WAVES, typename Length>
 __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedShared<T, HD>& sh, const Lengths& lengths, Length length) {
     typedef PagedShape<T, HD> P;
     constexpr int R = P::R, KT = P::KT, RG = P::RG, NK = P::NK, ND = P::ND, U = P::U, QE = P::QE, CH = WAVES ? P::TR : P::CH;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int H = a.H_kv * a.group, tiles = (a.group + kPagedHeads - 1) / kPagedHeads, HH = a.H_kv * tiles, GP = min(a.group, kPagedHeads);
     const Divisor& by_runs = WAVES ? a.by_waves : a.by_runs;
 
@@ -288,11 +288,18 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
     const bool out_whole = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && a.out_stride % 4 == 0;
 
     while (u < end) {
+        // 8 bits: what the loads of a (sequence, heads) need of the lane's number is computed here, not ahead of all of them, where it would be kept and others spilled
+        int self = tid, zero = 0;
+        if constexpr (P::ES == 1) {
+            asm volatile("" : "+v"(self));
+            asm volatile("" : "+s"(zero));
+        }
+        const int lane = self & 63, i = lane & 15, g = lane >> 4;
         const int chunks = chunks_of(len), per_head = chunks + over, hh = small_quotient(u - seq_begin, per_head), head_begin = seq_begin + hh * per_head;
         const int c0 = max(u - head_begin - over, 0), c1 = min(chunks, end - head_begin - over);
         const int next = min(end, head_begin + per_head);
         if (c1 <= 0) return;                                        // the run ends in what this one counts more
-        const int kvh = tiles == 1 ? hh : small_quotient(hh, tiles), h0 = (hh - kvh * tiles) * kPagedHeads, nh = min(kPagedHeads, a.group - h0);
+        const int kvh = tiles == 1 ? hh : small_quotient(hh, tiles + zero), h0 = (hh - kvh * tiles) * kPagedHeads, nh = min(kPagedHeads, a.group - h0);
         const bool whole = c0 == 0 && c1 == chunks;
         const int newest = len - 1, last_block = newest / R;
         const int* tab = a.tables + (size_t)b * a.table_stride;
@@ -359,17 +366,16 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
             int pk[U], pv[U], pk1[U], pv1[U], new_page = 0;
             load_pages(r, pk, pv);
             if (fresh) new_page = tab[last_block >> block_shift];
-            // (one 16-byte piece a lane, 64 dims in 8 bits: the dims with which a lane's turn are another lane's, so it loads these too)
-            constexpr int NQ = NK == 1 ? 2 : NK;
-            float qf[NQ][QE];
-            ActVec<QE, A> qa[NQ];
+            float qf[NK][QE];
+            ActVec<QE, A> qa[NK];
 #pragma unroll
-            for (int k = 0; k < NQ; ++k) qa[k].load(static_cast<const A*>(a.q) + b * a.q_stride + (long long)(kvh * a.group + h0 + min(i, nh - 1)) * HD + (NK == 1 ? (k == 0 ? g : g ^ 2) * QE : k * 4 * QE + g * QE));
-            // a lane has dims k * 4 QE + g * QE ... of q, k < NK: those half a head away, with which they turn, among them
-            ActVec<2 * QE, float> cs[NQ / 2];
+            for (int k = 0; k < NK; ++k) qa[k].load(static_cast<const A*>(a.q) + b * a.q_stride + (long long)(kvh * a.group + h0 + min(i, nh - 1)) * HD + k * 4 * QE + g * QE);
+            // a lane has dims k * 4 QE + g * QE ... of q, k < NK: those half a head away, with which they turn, among them (of one piece, 64 dims in 8 bits, they are lane ^ 32's)
+            constexpr int NC = NK == 1 ? 1 : NK / 2;
+            ActVec<2 * QE, float> cs[NC];
             if (a.rope_cs) {
 #pragma unroll
-                for (int k = 0; k < NQ / 2; ++k) cs[k].load(reinterpret_cast<const float*>(a.rope_cs + (size_t)b * (HD / 2) + (NK == 1 ? (g & 1) * QE : k * 4 * QE + g * QE)));
+                for (int k = 0; k < NC; ++k) cs[k].load(reinterpret_cast<const float*>(a.rope_cs + (size_t)b * (HD / 2) + (NK == 1 ? (g & 1) * QE : k * 4 * QE + g * QE)));
             }
             load_pages(after(r), pk1, pv1);
             A nk[2], nv[2];                                         // dims `lane` and lane + HD / 2 of the newest row
@@ -453,26 +459,28 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 }
             }
 #pragma unroll
-            for (int k = 0; k < NQ; ++k) qa[k].get(a.dtype, qf[k]);
+            for (int k = 0; k < NK; ++k) qa[k].get(a.dtype, qf[k]);
             if (a.rope_cs) {
 #pragma unroll
-                for (int k = 0; k < NQ / 2; ++k) {
+                for (int k = 0; k < NC; ++k) {
                     float c[2 * QE];
                     cs[k].get(D3_F32, c);
 #pragma unroll
                     for (int e = 0; e < QE; ++e) {
-                        if constexpr (NK == 1) {                    // own dims in the lower half of the head for g < 2
-                            qf[0][e] = g < 2 ? qf[0][e] * c[2 * e] - qf[1][e] * c[2 * e + 1] : qf[0][e] * c[2 * e] + qf[1][e] * c[2 * e + 1];
-                            continue;
+                        if constexpr (NK == 1) {
+                            const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(qf[0][e]), __float_as_uint(qf[0][e]), false, false);
+                            const float lo = __uint_as_float(both[0]), hi = __uint_as_float(both[1]);
+                            qf[0][e] = g < 2 ? lo * c[2 * e] - hi * c[2 * e + 1] : hi * c[2 * e] + lo * c[2 * e + 1];
+                        } else {
+                            const float lo = qf[k][e], hi = qf[k + NC][e];
+                            qf[k][e] = lo * c[2 * e] - hi * c[2 * e + 1];
+                            qf[k + NC][e] = hi * c[2 * e] + lo * c[2 * e + 1];
                         }
-                        const float lo = qf[k][e], hi = qf[k + NQ / 2][e];
-                        qf[k][e] = lo * c[2 * e] - hi * c[2 * e + 1];
-                        qf[k + NQ / 2][e] = hi * c[2 * e] + lo * c[2 * e + 1];
                     }
                 }
             }
             // q as fp16 halves hi + lo, scaled by a power of two that puts its largest element at 2^14: 22 bits of it
-            float mul = a.scale * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
+            float mul = (P::ES == 1 ? fabsf(a.scale) : a.scale) * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
             // In LDS from here on (where this wave puts its outputs in the end): in registers it would leave too few for the rows in flight.
             uint4* const q_lds = reinterpret_cast<uint4*>(sh.o[wave]) + lane;
             if constexpr (P::ES <= 2) {
@@ -486,7 +494,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
 #pragma unroll
                 for (int k = 0; k < NK; ++k) {
 #pragma unroll
-                    for (int e = 0; e < QE; ++e) qf[k][e] = __builtin_ldexpf(qf[k][e], ex);
+                    for (int e = 0; e < QE; ++e) qf[k][e] = __builtin_ldexpf(P::ES == 1 && a.scale < 0.f ? -qf[k][e] : qf[k][e], ex);
 #pragma unroll
                     for (int e = 0; e < QE; e += 8) {
                         float part[8];
@@ -519,7 +527,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                     for (int x = 0; x < U; ++x)
 #pragma unroll
                         for (int t = 0; t < KT; ++t) {
-                            if (r + x * RG + R * (i >> 2) + 4 * t + (i & 3) != newest) continue;
+                            if (newest - r - x * RG - R * (i >> 2) - (i & 3) != 4 * t) continue;
 #pragma unroll
                             for (int k = 0; k < NK; ++k) __builtin_memcpy(&kr[x][t][k], &sh.new_k[wave][k * 4 * QE + g * QE], 16);
                         }
@@ -532,6 +540,25 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
 #pragma unroll
                 for (int k = 0; k < P::QP; ++k) qr[k] = q_at[k * 64];
                 float s[U][R];
+                if constexpr (P::ES == 1) {
+                    // hi and lo in one sum a tile, a group's tiles side by side; scores stay in units of 1 / mul until they are exponents (mul > 0)
+#pragma unroll
+                    for (int x = 0; x < U; ++x) {
+                        if (with_new && r + x * RG + lane == newest) ksr[x] = new_ks;
+                        f32x4 d[KT] = {};
+#pragma unroll
+                        for (int k = 0; k < NK; ++k) {
+                            half8 kv[KT][2];
+#pragma unroll
+                            for (int t = 0; t < KT; ++t) decode16<T>(kr[x][t][k], kv[t]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                for (int t = 0; t < KT; ++t) d[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv[t][e / 2], __builtin_bit_cast(half8, qr[4 * k + e]), d[t], 0, 0, 0);
+                        }
+                        of_rows(ksr[x], [&](int e, float scale) { s[x][e] = d[e / 4][e % 4] * scale; });
+                    }
+                } else
 #pragma unroll
                 for (int x = 0; x < U; ++x)
 #pragma unroll
@@ -539,15 +566,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                         f32x4 d = {0.f, 0.f, 0.f, 0.f}, d1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int k = 0; k < NK; ++k) {
-                            if constexpr (P::ES == 1) {
-                                half8 kv[2];
-                                decode16<T>(kr[x][t][k], kv);
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv[e], __builtin_bit_cast(half8, qr[4 * k + 2 * e]), d, 0, 0, 0);
-                                    d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv[e], __builtin_bit_cast(half8, qr[4 * k + 2 * e + 1]), d1, 0, 0, 0);
-                                }
-                            } else if constexpr (P::ES == 2) {
+                            if constexpr (P::ES == 2) {
                                 const half8 kv = __builtin_bit_cast(half8, kr[x][t][k]);
                                 d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, __builtin_bit_cast(half8, qr[2 * k]), d, 0, 0, 0);
                                 d1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv, __builtin_bit_cast(half8, qr[2 * k + 1]), d1, 0, 0, 0);
@@ -562,15 +581,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                         }
 #pragma unroll
                         for (int j = 0; j < 4; ++j) s[x][4 * t + j] = (d[j] + d1[j]) * mul;
-                        if constexpr (P::ES == 1) __builtin_amdgcn_sched_barrier(0);
                     }
-                if constexpr (P::ES == 1) {
-#pragma unroll
-                    for (int x = 0; x < U; ++x) {
-                        if (with_new && r + x * RG + lane == newest) ksr[x] = new_ks;
-                        of_rows(ksr[x], [&](int e, float scale) { s[x][e] *= scale; });
-                    }
-                }
                 __builtin_amdgcn_sched_barrier(0);
                 int pk2[U], pv2[U];
                 if constexpr (MORE) {
@@ -580,10 +591,11 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 __builtin_amdgcn_sched_barrier(0);
                 if (tail || absent) {
 #pragma unroll
-                    for (int x = 0; x < U; ++x)
+                    for (int x = 0; x < U; ++x) {
+                        const int left = present(pv[x]) ? len - r - x * RG - R * g : 0;         // of the lane's R rows those that count
 #pragma unroll
-                        for (int e = 0; e < R; ++e)
-                            if (!present(pv[x]) || r + x * RG + R * g + e >= len) s[x][e] = -INFINITY;
+                        for (int e = 0; e < R; ++e) if (e >= left) s[x][e] = -INFINITY;
+                    }
                 }
                 // ---- running softmax of head i over the lane's rows (and, for the maximum, those of the other lanes that have the head) ----
                 float top = s[0][0];
@@ -591,6 +603,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 for (int x = 0; x < U; ++x)
 #pragma unroll
                     for (int e = 0; e < R; ++e) top = fmaxf(top, s[x][e]);
+                if constexpr (P::ES == 1) top *= mul;
                 top = fmaxf(m, reduce_halves(reduce_row_pairs(top, MaxOp()), MaxOp()));
                 if (__any(top > m)) {
                     const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
@@ -607,7 +620,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 for (int x = 0; x < U; ++x)
 #pragma unroll
                     for (int e = 0; e < R; ++e) {
-                        s[x][e] = __builtin_amdgcn_exp2f(s[x][e] - sub);
+                        s[x][e] = __builtin_amdgcn_exp2f(P::ES == 1 ? fmaf(s[x][e], mul, -sub) : s[x][e] - sub);
                         l += s[x][e];
                     }
                 if constexpr (P::ES == 1) {
@@ -641,15 +654,15 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                     constexpr uint32_t ROW = PER == 4 ? 0xffu : PER == 2 ? 0xffffu : 0xffffffffu;
 #pragma unroll
                     for (int x = 0; x < U; ++x) {
-                        const int row0 = r + x * RG + R * g;
+                        const int left = present(pv[x]) ? len - r - x * RG - R * g : 0, fresh_at = newest - r - x * RG - R * g;
                         uint32_t counts[4], fresh_bits[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             counts[j] = fresh_bits[j] = 0;
 #pragma unroll
                             for (int e = 0; e < PER; ++e) {
-                                counts[j] |= present(pv[x]) && row0 + j * PER + e < len ? ROW << (8 * P::ES * e) : 0u;
-                                fresh_bits[j] |= row0 + j * PER + e == newest ? ROW << (8 * P::ES * e) : 0u;
+                                counts[j] |= j * PER + e < left ? ROW << (8 * P::ES * e) : 0u;
+                                fresh_bits[j] |= j * PER + e == fresh_at ? ROW << (8 * P::ES * e) : 0u;
                             }
                         }
                         if (with_new) {                             // the newest row's value takes its place
@@ -674,6 +687,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
 #pragma unroll
                 for (int x = 0; x < U; ++x) {
                     if constexpr (P::ES == 1) {
+                        __builtin_amdgcn_sched_barrier(0);
                         half8 ph[2], pl[2];
 #pragma unroll
                         for (int e = 0; e < 2; ++e) {
@@ -682,15 +696,15 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                             split_half8(part, ph[e], pl[e]);
                         }
 #pragma unroll
-                        for (int d = 0; d < ND; ++d) {
-                            half8 v[2];
-                            decode16<T>(vr[x][d], v);
+                        for (int d0 = 0; d0 < ND; d0 += 4) {        // four sums side by side: a product waits for the one before it of its own sum
+                            half8 v[4][2];
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[e], ph[e], acc[d], 0, 0, 0);
-                                acc[d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[e], pl[e], acc[d], 0, 0, 0);
-                            }
-                            if (d % 2) __builtin_amdgcn_sched_barrier(0);
+                            for (int d = 0; d < 4; ++d) decode16<T>(vr[x][d0 + d], v[d]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                for (int d = 0; d < 4; ++d) acc[d0 + d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[d][e / 2], e % 2 ? pl[e / 2] : ph[e / 2], acc[d0 + d], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);
                         }
                     } else if constexpr (P::ES == 2) {
                         half8 ph, pl;
@@ -741,8 +755,8 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
         // Partial results of a (sequence, heads) are those of runs w0 .. w1.  A run has at most two: in slot 2 run of the one that it begins in, in the next of the one that it ends in.
         int w0 = run, parts = 1;
         if (!whole) {
-            w0 = runs.of(head_begin + over);
-            parts = runs.of(head_begin + per_head - 1) - w0 + 1;
+            w0 = runs.of(head_begin + over, P::ES == 1 ? none : 0);
+            parts = runs.of(head_begin + per_head - 1, P::ES == 1 ? none : 0) - w0 + 1;
         }
         const unsigned before = runs.begin(w0) < head_begin ? 1 : 0;
         auto slot_of = [&](int k) { return 2u * (w0 + k) + (k == 0 ? before : 0); };

@@ -17,7 +17,7 @@ struct i8_t { uint8_t bits; };             // two's complement
 struct e4m3_t { uint8_t bits; };           // sign, 4 bits of exponent, 3 of mantissa, bias 7; no infinities
 
 constexpr float kScaledMost = 3e38f, kScaledLeast = 0x1p-100f;
-template <typename T> struct MostCode;
+template <typename T> struct MostCode { static constexpr float value = 0.f; };
 template <> struct MostCode<i8_t> { static constexpr float value = 127.f; };
 template <> struct MostCode<e4m3_t> { static constexpr float value = 448.f; };
 

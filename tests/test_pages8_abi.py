@@ -58,3 +58,16 @@ def test_a_context_has_no_cache_of_8_bits(lib):
     for kv in (binding.D3_I8, binding.D3_E4M3):
         d = binding._ModelDesc(2, 256, 4, 4, 64, 512, 1000, 1e-6, 10000.0, binding.D3_F32, kv, 1, 64)
         assert lib.d3_workspace_size(C.byref(d)) == 0
+
+
+@pytest.mark.parametrize("source,kernel,count", [("attention_paged8.hip", "attn_paged_kernel", 16), ("pages8.hip", "pages_", 36)])
+def test_kernels_use_no_scratch(tmp_path, source, kernel, count):
+    """A kernel with any scratch at all starts 1 us later, and the attention's loop over rows takes up to twice as long with spills in it; nothing else shows either."""
+    out = str(tmp_path / "k.s")
+    flags = [f for f in d3_build.FLAGS if f != "-fPIC"]
+    subprocess.run([d3_build.HIPCC] + flags + ["-x", "hip", "-S", "--offload-device-only", os.path.join(d3_build.CSRC, source), "-o", out], check=True, capture_output=True)
+    text = open(out).read()
+    assert len(set(re.findall(r"\.name:\s+(\S*" + kernel + r"\S*)", text))) == count
+    for field, most in ((".private_segment_fixed_size", 0), (".vgpr_spill_count", 0), (".vgpr_count", 256)):
+        found = [int(x) for x in re.findall(re.escape(field) + r":\s+(\d+)", text)]
+        assert len(found) == count and max(found) <= most, (field, found)
