@@ -133,15 +133,6 @@ __device__ __forceinline__ void decode16(const uint4& w, half8 (&y)[2]) {
         y[j / 2][j % 2 * 4 + 2] = hi[0]; y[j / 2][j % 2 * 4 + 3] = hi[1];
     }
 }
-// f(e, v of lane e) of the 16 lanes of this lane's row of lanes: an operand of the instruction that uses it
-template <int E = 0, typename F>
-__device__ __forceinline__ void of_rows(float v, F f) {
-    if constexpr (E < 16) {
-        f(E, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + E, 0xf, 0xf, false)));
-        of_rows<E + 1>(v, f);
-    }
-}
-
 // st_agent, ld_agent of two adjacent floats
 __device__ __forceinline__ void st_agent2(float* p, float x, float y) {
     __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);

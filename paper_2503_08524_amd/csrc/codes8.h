@@ -27,6 +27,15 @@ struct MaxMagnitude {
 };
 __device__ __forceinline__ float magnitude(float x) { return __uint_as_float(__float_as_uint(x) & 0x7fffffffu); }
 
+// f(e, v of lane e) of the 16 lanes of this lane's row of lanes: an operand of the instruction that uses it
+template <int E = 0, typename F>
+__device__ __forceinline__ void of_rows(float v, F f) {
+    if constexpr (E < 16) {
+        f(E, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + E, 0xf, 0xf, false)));
+        of_rows<E + 1>(v, f);
+    }
+}
+
 struct RowScale { float scale, inv; };     // value = code * scale, code = value * inv
 template <typename T>
 __device__ __forceinline__ RowScale row_scale(float most) {
@@ -63,13 +72,6 @@ __device__ __forceinline__ void encode(const float (&x)[N], uint32_t (&w)[(N + 3
         }
     }
 }
-template <typename T> __device__ __forceinline__ T encode1(float x) {
-    const float two[2] = {x, x};
-    uint32_t w[1];
-    encode<T, 2>(two, w);
-    return T{(uint8_t)w[0]};
-}
-
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 // The four codes of a word as fp16, which holds every code of either type.  i8: the bytes with their signs turned over are the last digits of 1024 + 0 ... 1024 + 255.
 template <typename T>

@@ -94,9 +94,29 @@ template <int N> __device__ __forceinline__ float reduce_lanes(float v) {
 #undef D3_FROM
     return v;
 }
-__device__ __forceinline__ float reduce_wave(float v) {
+// Of 16 rows at once, a lane's part of each in m: lane l gets that of row l % 16.  In each of four steps a lane keeps half of its rows and takes its partner's part of these (15 exchanges; row by row it is 96);
+// the lanes l ^ 8, l ^ 7, l ^ 2 and l ^ 1 that they exchange with make up the 16 side by side, and two steps more the wave.
+__device__ __forceinline__ float reduce_rows16(const float (&m)[16], int lane) {
     const MaxMagnitude op;
-    return reduce_halves(reduce_row_pairs(reduce_row(v, op), op), op);
+    float a[8], b[4], c[2];
+#define D3_FROM(v, ctrl) __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, 0xf, 0xf, false))
+#define D3_HALF(to, from, n, bit, ctrl)                                          \
+    _Pragma("unroll") for (int e = 0; e < n; ++e) {                              \
+        const float keep = lane & bit ? from[e + n] : from[e], give = lane & bit ? from[e] : from[e + n]; \
+        to[e] = op(keep, D3_FROM(give, ctrl));                                   \
+    }
+    D3_HALF(a, m, 8, 8, 0x128)
+    D3_HALF(b, a, 4, 4, 0x141)
+    D3_HALF(c, b, 2, 2, 0x4e)
+    const float keep = lane & 1 ? c[1] : c[0], give = lane & 1 ? c[0] : c[1];
+    const float d = op(keep, D3_FROM(give, 0xb1));
+#undef D3_HALF
+#undef D3_FROM
+    return reduce_halves(reduce_row_pairs(d, op), op);
+}
+
+__device__ __forceinline__ unsigned long long lane_of(unsigned long long v, int lane) {
+    return (unsigned long long)(unsigned)__builtin_amdgcn_readlane((unsigned)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((unsigned)v, lane);
 }
 
 // The tokens that a wave looks at for its own WN, R - 1 before them (lane 0 is the first of these) to R - 1 behind, as the slots of values lie in units of R rows.
@@ -184,61 +204,55 @@ __global__ __launch_bounds__(256) void pages_append8_kernel(AppendArgs a) {
     }
     const int t0 = (blockIdx.x * 4 + wave) * kValueTokens;
     if (t0 >= a.n) return;
+    // the rows of the wave's own tokens, requested beside their slots; those of a unit that begins among them, where it does not begin with the first
+    Vec<DL, S> v[R];
+    auto load_rows = [&](int first) {
+#pragma unroll
+        for (int e = 0; e < R; ++e) v[e].load(src + min(first + e, a.n - 1) * a.token_stride + lane * DL);
+    };
+    load_rows(t0);
+    const int own = lane < R ? slot_at(t0 + lane) : -1;
     const Units<R, kValueTokens> units(lane, t0, slot_at);
-    auto load_rows = [&](auto count, int first, float (&y)[decltype(count)::value][DL], float (&most)[decltype(count)::value]) {
-        constexpr int N = decltype(count)::value;
-        Vec<DL, S> v[N];
+    const int unit_at = units.firsts ? __builtin_ctzll(units.firsts) - (R - 1) : 0;        // one at most: units begin 16 tokens apart
+#pragma unroll 1
+    for (int pass = units.singles ? 0 : 1; pass < (units.firsts ? 2 : 1); ++pass) {
+        if (pass == 1 && unit_at != 0) load_rows(t0 + unit_at);
+        float y[R][DL], most[R];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e].load(src + min(first + e, a.n - 1) * a.token_stride + lane * DL);
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
+        for (int e = 0; e < R; ++e) {
             v[e].get(y[e]);
             most[e] = magnitude(y[e][0]);
             if (DL == 2) most[e] = MaxMagnitude()(most[e], magnitude(y[e][DL - 1]));
         }
+        const RowScale s = row_scale<T>(reduce_rows16(most, lane));                    // of row lane % 16
+        of_rows(s.inv, [&](int e, float inv) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) most[e] = reduce_wave(most[e]);
-    };
-    if (units.firsts) {                                             // one at most: units begin 16 tokens apart
-        const int x = __builtin_ctzll(units.firsts), at = __builtin_amdgcn_readlane(units.slot, x);
-        float y[R][DL], most[R], scale = 0.f;
-        load_rows(std::integral_constant<int, R>(), t0 - (R - 1) + x, y, most);
-#pragma unroll
-        for (int e = 0; e < R; ++e) {
-            const RowScale s = row_scale<T>(most[e]);
-            if (lane == e) scale = s.scale;
-#pragma unroll
-            for (int d = 0; d < DL; ++d) y[e][d] *= s.inv;
-        }
-        const size_t row = rows_at(at) + (at & row_mask);
-        char* to = pool + row * HD + lane * (DL * R);
+            for (int d = 0; d < DL; ++d) y[e][d] *= inv;
+        });
+        Vec<4, float> w[DL];
 #pragma unroll
         for (int d = 0; d < DL; ++d) {
             float z[R];
 #pragma unroll
             for (int e = 0; e < R; ++e) z[e] = y[e][d];
-            Vec<4, float> w;
-            encode<T, R>(z, w.w);
-            w.store(to + d * R);
+            encode<T, R>(z, w[d].w);
         }
-        if (lane < R) scales[row + lane] = scale;
-    }
-#pragma unroll 1
-    for (int part = 0; part < kValueTokens; part += 8) {
-        const unsigned need = (unsigned)(units.singles >> part) & 0xffu;
-        if (!need) continue;
-        float y[8][DL], most[8];
-        load_rows(std::integral_constant<int, 8>(), t0 + part, y, most);
+        if (pass == 1) {
+            const int at = __builtin_amdgcn_readlane(units.slot, R - 1 + unit_at);
+            const size_t row = rows_at(at) + (at & row_mask);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if (!(need >> e & 1)) continue;
-            const int at = __builtin_amdgcn_readlane(units.slot, R - 1 + part + e);
-            const RowScale s = row_scale<T>(most[e]);
-            const size_t head = rows_at(at);
-            uint8_t* to = reinterpret_cast<uint8_t*>(pool) + head * HD + (size_t)((at & row_mask) / R * HD + lane * DL) * R + at % R;
+            for (int d = 0; d < DL; ++d) w[d].store(pool + row * HD + (lane * DL + d) * R);
+            if (lane < R) scales[row + lane] = s.scale;
+        } else {
+            const unsigned long long row = rows_at(own) + (own & row_mask), at = (row & ~(unsigned long long)(R - 1)) * HD + own % R;       // (means nothing where the token is none)
 #pragma unroll
-            for (int d = 0; d < DL; ++d) to[d * R] = encode1<T>(y[e][d] * s.inv).bits;
-            if (lane == 0) scales[head + (at & row_mask)] = s.scale;
+            for (int e = 0; e < R; ++e) {
+                if (!(units.singles >> e & 1)) continue;
+                char* to = pool + lane_of(at, e) + lane * (DL * R);
+#pragma unroll
+                for (int d = 0; d < DL; ++d) to[d * R] = (char)(w[d].w[e / 4] >> (8 * (e % 4)));
+            }
+            if (units.singles >> lane & 1) scales[row] = s.scale;          // (no bits from R on)
         }
     }
 }
@@ -247,7 +261,7 @@ __global__ __launch_bounds__(256) void pages_append8_kernel(AppendArgs a) {
 // grid as above.  Where R tokens are a unit of R rows, a wave reads the unit's 16 bytes per dim and writes the R rows; elsewhere it reads elements.
 template <typename T, typename D, int HD>
 __global__ __launch_bounds__(256) void pages_read_kernel(ReadArgs a) {
-    constexpr int R = 16 / sizeof(T), DL = HD / 64, WN = kTokens / 4;
+    constexpr int R = 16 / sizeof(T), DL = HD / 64, WN = R == 16 ? 16 : 8;          // tokens of a wave: of values
     constexpr bool SCALED = sizeof(T) == 1;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = blockIdx.y, layer = blockIdx.z >> 1;
     const bool values = blockIdx.z & 1;
@@ -289,7 +303,9 @@ __global__ __launch_bounds__(256) void pages_read_kernel(ReadArgs a) {
         }
         return;
     }
-    const int t0 = blockIdx.x * kTokens + wave * WN;
+    const int t0 = (blockIdx.x * 4 + wave) * WN;
+    if (t0 >= a.n) return;
+    const int own = lane < WN ? slot_at(t0 + lane) : -1;
     const Units<R, WN> units(lane, t0, slot_at);
     for (unsigned long long left = units.firsts; left; left &= left - 1) {
         const int x = __builtin_ctzll(left), at = __builtin_amdgcn_readlane(units.slot, x);
@@ -315,24 +331,32 @@ __global__ __launch_bounds__(256) void pages_read_kernel(ReadArgs a) {
             w.store(to + e * a.token_stride);
         }
     }
-    for (unsigned left = (unsigned)units.singles; left; left &= left - 1) {
-        const int x = __builtin_ctz(left), at = __builtin_amdgcn_readlane(units.slot, R - 1 + x);
-        const size_t head = rows_at(at);
-        Vec<1, T> in[DL];
-        float z[DL];
-        const char* from = pool + (head * HD + (size_t)((at & row_mask) / R * HD + lane * DL) * R + at % R) * sizeof(T);
+    if (!units.singles) return;
+    Vec<1, T> in[WN][DL];
+    float scale = 0.f;                                              // of row `lane`
+    const int from = max(own, 0);                                   // (tokens that are in a unit, or none, are loaded too)
+    const unsigned long long row = rows_at(from) + (from & row_mask), at = ((row & ~(unsigned long long)(R - 1)) * HD + from % R) * sizeof(T);
+    if (SCALED) scale = scales[row];
 #pragma unroll
-        for (int d = 0; d < DL; ++d) in[d].load(from + d * 16);
-        const float scale = SCALED ? scales[head + (at & row_mask)] : 1.f;
+    for (int e = 0; e < WN; ++e) {
+        const char* p = pool + lane_of(at, e) + lane * (DL * 16);
+#pragma unroll
+        for (int d = 0; d < DL; ++d) in[e][d].load(p + d * 16);
+    }
+#pragma unroll
+    for (int e = 0; e < WN; ++e) {
+        if (!(units.singles >> e & 1)) continue;
+        const float by = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale), e));
+        float z[DL];
 #pragma unroll
         for (int d = 0; d < DL; ++d) {
             float y[1];
-            in[d].get(y);
-            z[d] = SCALED ? value_of(y[0], scale) : y[0];
+            in[e][d].get(y);
+            z[d] = SCALED ? value_of(y[0], by) : y[0];
         }
         Vec<DL, D> w;
         w.put(z);
-        w.store(out + (long long)(t0 + x) * a.token_stride + lane * DL);
+        w.store(out + (t0 + e) * a.token_stride + lane * DL);
     }
 }
 
