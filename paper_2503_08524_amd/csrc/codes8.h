@@ -54,24 +54,31 @@ __device__ __forceinline__ void turned(float& lo, float& hi, float2 cs) {
     hi = c + d;
 }
 
-// N codes (2 or a multiple of 4) of values x already multiplied by inv, in order from the lowest byte
+// N codes (2 or a multiple of 4) of values x already multiplied by inv, in order from the lowest byte.  The bounds are for infinities.  Whole numbers: the last byte of 1.5 2^23 + x is x to nearest even, as long as
+// the product that x is has been rounded by itself.
 template <typename T, int N>
 __device__ __forceinline__ void encode(const float (&x)[N], uint32_t (&w)[(N + 3) / 4]) {
+#pragma clang fp contract(off)
     constexpr float Q = MostCode<T>::value;
-    auto bound = [](float v) { return fmaxf(fminf(v, Q), -Q); };
+    constexpr int PER = N < 4 ? N : 4;
 #pragma unroll
     for (int j = 0; j < (N + 3) / 4; ++j) {
-        constexpr int PER = N < 4 ? N : 4;
-        w[j] = 0;
-        if constexpr (sizeof(T) == 1 && MostCode<T>::value == 127.f) {
+        float y[PER];
 #pragma unroll
-            for (int e = 0; e < PER; ++e) w[j] |= ((uint32_t)(int)rintf(bound(x[4 * j + e])) & 0xffu) << (8 * e);
+        for (int e = 0; e < PER; ++e) y[e] = __builtin_amdgcn_fmed3f(x[4 * j + e], -Q, Q);
+        if constexpr (Q == 127.f) {
+            uint32_t b[PER];
+#pragma unroll
+            for (int e = 0; e < PER; ++e) b[e] = __float_as_uint(y[e] + 12582912.f);
+            w[j] = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u);
+            if constexpr (PER == 4) w[j] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), w[j], 0x05040100u);
         } else {
-            w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(bound(x[4 * j]), bound(x[4 * j + 1]), w[j], false);
-            if constexpr (PER == 4) w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(bound(x[4 * j + 2]), bound(x[4 * j + 3]), w[j], true);
+            w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+            if constexpr (PER == 4) w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w[j], true);
         }
     }
 }
+
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 // The four codes of a word as fp16, which holds every code of either type.  i8: the bytes with their signs turned over are the last digits of 1024 + 0 ... 1024 + 255.
 template <typename T>
