@@ -423,14 +423,16 @@ class PagedCache:
 
     def _rows(self, slots, k, v):
         """(layers, rows, type, strides of row, head and layer) of k and v for append and read."""
-        self._ints(slots=slots)
-        n, kind = slots.numel(), self._kind(k)
+        if slots.dtype is not self._int32 or slots.get_device() != self._index or not slots.is_contiguous():
+            self._ints(slots=slots)
+        n, kind, dtype, heads = slots.numel(), self._kind(k), k.dtype, self.n_kv_heads
         layers = k.shape[0] if k.dim() == 4 else 1
-        dims = (layers, n, self.n_kv_heads, self.head_dim) if k.dim() == 4 else (n, self.n_kv_heads, self.head_dim)
-        strides = self._heads("k", k, dims, k.dtype)
-        self._heads("v", v, dims, k.dtype, strides)
+        dims = (layers, n, heads, self.head_dim) if k.dim() == 4 else (n, heads, self.head_dim)
+        strides = self._heads("k", k, dims, dtype)
+        if v.stride() != strides or v.shape != dims or v.dtype is not dtype or v.get_device() != self._index:       # (else it is k's like)
+            self._heads("v", v, dims, dtype, strides)
         # (the stride of a dim with one entry says nothing)
-        return layers, n, kind, (strides[-3] if n > 1 else 0, strides[-2] if self.n_kv_heads > 1 else 0, strides[0] if layers > 1 else 0)
+        return layers, n, kind, (strides[-3] if n > 1 else 0, strides[-2] if heads > 1 else 0, strides[0] if layers > 1 else 0)
 
     def _kind(self, t) -> int:
         kind = self._kinds.get(t.dtype)

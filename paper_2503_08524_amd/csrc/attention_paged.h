@@ -7,6 +7,8 @@
 // knows no lengths, so a launch can be captured once and replayed while sequences grow.  A run that covers a (sequence, heads) whole writes the
 // result; else it publishes (max, sum, unnormalised output), and the run that arrives last joins them.
 //
+// Rows of 8 bits (codes8.h) come with a scale for each row: see attention_paged8.hip for what they add.
+//
 // Both contractions run on the matrix cores with the query heads of a KV head as one matrix dimension, straight from the registers that the
 // loads fill (see pages.h for the layout of the values):
 //   scores  D[row][head] = K[row][dim] q[head][dim]: a lane (i = lane % 16, g = lane / 16) loads 16 bytes of row i and ends with the scores of head i for

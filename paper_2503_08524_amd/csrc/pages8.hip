@@ -1,4 +1,4 @@
-// Rows into pages of 8 bits, quantised as they are written, and rows out of pages of any type.
+// Rows into pages of 8 bits, quantised as they are written (codes8.h), and rows out of pages of any type.  Both move every byte once and are bound by memory, or by a launch where there are few rows: see kTokens.
 #include <algorithm>
 #include <type_traits>
 
