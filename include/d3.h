@@ -244,10 +244,11 @@ int d3_truncate(d3_ctx *ctx, int32_t n_rows);
  * row's norm where its dims are alike: such caches are for callers who take that for half the bytes.  Where one dim is many times the others D3_I8 leaves those few codes, D3_E4M3 as many digits as before.
  * A page number outside
  * [0, n_pages) in a table is a page that is not there: its rows count as masked.  A slot outside the pool is skipped.
- * A row may be given to one slot at a time (two rows of one call with the same slot: either is kept, element by element).
+ * A row may be given to one slot at a time (two rows of one call with the same slot: either is kept, element by element; in pools of 8 bits the codes of one may
+ * meet the scale of the other, and the row means nothing).
  * Calls on one d3_pages must be ordered (one stream, or streams that wait for each other; replays of graphs too): they share
  * its workspace, and they read what the ones before wrote.  Two handles on the same pools, each with a workspace of its own, may
- * be used at the same time as far as neither writes what the other reads. */
+ * be used at the same time as far as neither writes what the other reads, nor both into one page of a layer (the newest value of an attention is written with its neighbours' 16 bytes). */
 typedef struct {
     int32_t n_layers, n_heads, n_kv_heads, head_dim;   /* head_dim 64 or 128; n_heads % n_kv_heads == 0 */
     int32_t kv_dtype;                                  /* D3_F16 or D3_F32, see d3_model_desc; D3_I8, D3_E4M3 */

@@ -473,7 +473,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 }
             }
             // q as fp16 halves hi + lo, scaled by a power of two that puts its largest element at 2^14: 22 bits of it
-            float mul = (P::ES == 1 ? fabsf(a.scale) : a.scale) * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
+            float mul = a.scale * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
             // In LDS from here on (where this wave puts its outputs in the end): in registers it would leave too few for the rows in flight.
             uint4* const q_lds = reinterpret_cast<uint4*>(sh.o[wave]) + lane;
             if constexpr (P::ES <= 2) {
@@ -487,7 +487,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
 #pragma unroll
                 for (int k = 0; k < NK; ++k) {
 #pragma unroll
-                    for (int e = 0; e < QE; ++e) qf[k][e] = __builtin_ldexpf(P::ES == 1 && a.scale < 0.f ? -qf[k][e] : qf[k][e], ex);
+                    for (int e = 0; e < QE; ++e) qf[k][e] = __builtin_ldexpf(qf[k][e], ex);
 #pragma unroll
                     for (int e = 0; e < QE; e += 8) {
                         float part[8];
@@ -534,7 +534,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 for (int k = 0; k < P::QP; ++k) qr[k] = q_at[k * 64];
                 float s[U][R];
                 if constexpr (P::ES == 1) {
-                    // hi and lo in one sum a tile, a group's tiles side by side; scores stay in units of 1 / mul until they are exponents (mul > 0)
+                    // hi and lo in one sum a tile, a group's tiles side by side; mul ahead of the row's scale, so that only a score that is too large for fp32 overflows
 #pragma unroll
                     for (int x = 0; x < U; ++x) {
                         if (with_new && r + x * RG + lane == newest) ksr[x] = new_ks;
@@ -549,7 +549,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
 #pragma unroll
                                 for (int t = 0; t < KT; ++t) d[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv[t][e / 2], __builtin_bit_cast(half8, qr[4 * k + e]), d[t], 0, 0, 0);
                         }
-                        of_rows(ksr[x], [&](int e, float scale) { s[x][e] = d[e / 4][e % 4] * scale; });
+                        of_rows(ksr[x], [&](int e, float scale) { s[x][e] = d[e / 4][e % 4] * mul * scale; });
                     }
                 } else
 #pragma unroll
@@ -596,7 +596,6 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 for (int x = 0; x < U; ++x)
 #pragma unroll
                     for (int e = 0; e < R; ++e) top = fmaxf(top, s[x][e]);
-                if constexpr (P::ES == 1) top *= mul;
                 top = fmaxf(m, reduce_halves(reduce_row_pairs(top, MaxOp()), MaxOp()));
                 if (__any(top > m)) {
                     const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
@@ -613,7 +612,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 for (int x = 0; x < U; ++x)
 #pragma unroll
                     for (int e = 0; e < R; ++e) {
-                        s[x][e] = __builtin_amdgcn_exp2f(P::ES == 1 ? fmaf(s[x][e], mul, -sub) : s[x][e] - sub);
+                        s[x][e] = __builtin_amdgcn_exp2f(s[x][e] - sub);
                         l += s[x][e];
                     }
                 if constexpr (P::ES == 1) {

@@ -584,6 +584,25 @@ def test_attention_large_scores():
                 assert ((out.double() - want).abs() <= 1e-5 * want.abs() + 1e-6).double().mean() > 0.9
 
 
+@pytest.mark.parametrize("kv", ["i8", "e4m3"])
+@pytest.mark.parametrize("keys,queries", [(1e-25, 1.0), (1e-25, 1e25), (1e20, 1e-20), (1e30, 1e-30), (1e33, 1.0), (1e36, 1.0), (3e36, 1e-36)])
+def test_attention_of_keys_and_queries_of_any_size(kv, keys, queries):
+    """Keys far from one: where the queries make up for them the outputs are those of ordinary ones, and where they do not the weights are all alike or 0 and 1; nothing but a score that is too large for
+    fp32 (sum |q k| is 1e38 at most here) would overflow."""
+    import torch
+    lens = [70, 300, 1000]
+    cache, g = _cache(lens, 2, 2, 128, kv, 16, seed=19, garbage=True)
+    cache.k_scales.mul_(keys)
+    q = torch.empty(3, 4, 128, device=DEV).normal_(generator=g) * queries
+    out = cache.attend(0, q)
+    want, most = _reference(cache, q.double(), lens)
+    if keys * queries < 100:
+        _check(out, want, most)
+    else:                                                   # rows whose scores are apart by more than fp32's error of the largest: all heads but those with a tie to that
+        assert out.isfinite().all()
+        assert ((out.double() - want).abs() <= 1e-5 * want.abs() + 1e-6).double().mean() > 0.9
+
+
 def test_attention_scale_layers_strides_and_an_output_with_gaps():
     import torch
     heads, group, hd, lens = 2, 2, 128, [40, 300, 0, 9]
