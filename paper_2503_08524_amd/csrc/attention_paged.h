@@ -650,6 +650,12 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                         uint32_t counts[4], fresh_bits[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
+                            if constexpr (P::ES == 1) {             // bytes 0 .. left - 1, and byte fresh_at, of 16
+                                const int n = max(left - 4 * j, 0);
+                                counts[j] = n >= 4 ? ~0u : (1u << (8 * n & 31)) - 1;
+                                fresh_bits[j] = fresh_at >> 2 == j ? 0xffu << (8 * fresh_at & 31) : 0u;
+                                continue;
+                            }
                             counts[j] = fresh_bits[j] = 0;
 #pragma unroll
                             for (int e = 0; e < PER; ++e) {
@@ -663,7 +669,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                                 uint32_t own = 0;
                                 __builtin_memcpy(&own, &sh.new_v[wave][d * 16 + i], P::ES);
                                 if (PER == 2) own |= own << 16;
-                                if (PER == 4) own *= 0x01010101u;
+                                if (PER == 4) own = __builtin_amdgcn_perm(own, own, 0u);
                                 vr[x][d].x = (fresh_bits[0] & own) | (~fresh_bits[0] & vr[x][d].x);
                                 vr[x][d].y = (fresh_bits[1] & own) | (~fresh_bits[1] & vr[x][d].y);
                                 vr[x][d].z = (fresh_bits[2] & own) | (~fresh_bits[2] & vr[x][d].z);
