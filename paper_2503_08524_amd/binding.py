@@ -265,7 +265,7 @@ class Decoder:
         _check(self.lib.d3_store_pages(self.ctx, cache.handle, seq, row_begin, slots.numel(), slots.data_ptr(), self._stream()))
 
     def decode_step_paged(self, cache: "PagedCache", tok_in, step_i: int, tok_out, logits=None, hidden_dump=None, starts=None) -> None:
-        """One step of the cache's first tok_in.numel() sequences, whose newest rows cache.reserve has made room for.  starts: what that reserve returned; the sequences
+        """One step of the cache's first tok_in.numel() sequences, whose newest rows cache.reserve has made room for; the cache is of this context's type or of 8 bits.  starts: what that reserve returned; the sequences
         that it gave no row (refused, paused, ended) are idle: their rows stay, tok_out is tok_in.  Without it every sequence that has rows must have got one, or
         the step overwrites its newest row.  fill_missing_paged of that reserve's slots comes next, before any step that runs a block this one drops."""
         cache._ints(tok_in=tok_in, tok_out=tok_out)

@@ -145,7 +145,7 @@ struct Units {
 // grid: (64 tokens, KV head, layer and half: keys or values).
 // A key is a row of its page: 16 bytes of the source's lower half and their partners per thread, the row's magnitude from the threads beside it.
 // Values: a wave has 16 tokens, a lane one or two dims of all of them; where 16 tokens fill a unit of 16 rows it writes the unit's 16 bytes per dim, elsewhere bytes.
-// Workgroups of 16 / 32 / 64 tokens, us: 512 rows of 32 heads, fp32 to e4m3 with rotation, 10.7 / 8.3 / 7.1; 8 layers x 1024 rows of 8 heads 26.0 / 24.1 / 17.8 (4.7 TB/s, a large copy's rate); 1024 rows of 40 heads,
+// Workgroups of 16 / 32 / 64 tokens, us (the shortest of 30 launches): 512 rows of 32 heads, fp32 to e4m3 with rotation, 10.7 / 8.3 / 7.1; 8 layers x 1024 rows of 8 heads 26.0 / 24.1 / 17.8 (4.7 TB/s, a large copy's rate); 1024 rows of 40 heads,
 // fp16 to i8, 15.8 / 12.8 / 10.5; read, 4 layers x 2304 rows of 32 heads, i8 to fp16, 55 / 47 / 40 (5.7 TB/s): workgroups begin one after the other, and the loads of four rounds are in flight together.
 constexpr int kTokens = 64, kValueTokens = kTokens / 4;
 
