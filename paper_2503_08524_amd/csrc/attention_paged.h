@@ -473,7 +473,8 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 }
             }
             // q as fp16 halves hi + lo, scaled by a power of two that puts its largest element at 2^14: 22 bits of it
-            float mul = a.scale * 1.4426950408889634f;               // scores are kept in units of log2(e): every exponential is one hardware exp2
+            float mul = (P::ES == 1 ? __builtin_amdgcn_frexp_mantf(a.scale) : a.scale) * 1.4426950408889634f;    // scores are kept in units of log2(e): every exponential is one hardware exp2
+            bool far = false;
             // In LDS from here on (where this wave puts its outputs in the end): in registers it would leave too few for the rows in flight.
             uint4* const q_lds = reinterpret_cast<uint4*>(sh.o[wave]) + lane;
             if constexpr (P::ES <= 2) {
@@ -499,7 +500,14 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                         q_lds[(at + 1) * 64] = __builtin_bit_cast(uint4, lo);
                     }
                 }
-                mul = __builtin_ldexpf(mul, -ex);
+                if constexpr (P::ES == 1) {
+                    // Codes have at most 2^31 in a product with q, and scales of rows 2^121: with 2^-120 to 2^95 ahead of the row's scale (all there is to it, but for queries or a scale far from one) mul is a normal
+                    // number and only a score that is too large for fp32 overflows.  The rest, `far`, goes by head into LDS, where sums come at the end, and is left out where no head has any.
+                    const int all = __builtin_amdgcn_frexp_expf(a.scale) - ex, near = min(max(all, -120), 95);
+                    mul = __builtin_ldexpf(mul, near);
+                    far = __any(all != near);
+                    if (g == 0) sh.l[i][wave] = __int_as_float(all - near);
+                } else mul = __builtin_ldexpf(mul, -ex);
             } else {
 #pragma unroll
                 for (int k = 0; k < NK; ++k) __builtin_memcpy(&q_lds[k * 64], qf[k], 16);
@@ -534,7 +542,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 for (int k = 0; k < P::QP; ++k) qr[k] = q_at[k * 64];
                 float s[U][R];
                 if constexpr (P::ES == 1) {
-                    // hi and lo in one sum a tile, a group's tiles side by side; mul ahead of the row's scale, so that only a score that is too large for fp32 overflows
+                    // hi and lo in one sum a tile, a group's tiles side by side; mul ahead of the row's scale
 #pragma unroll
                     for (int x = 0; x < U; ++x) {
                         if (with_new && r + x * RG + lane == newest) ksr[x] = new_ks;
@@ -550,6 +558,13 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                                 for (int t = 0; t < KT; ++t) d[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kv[t][e / 2], __builtin_bit_cast(half8, qr[4 * k + e]), d[t], 0, 0, 0);
                         }
                         of_rows(ksr[x], [&](int e, float scale) { s[x][e] = d[e / 4][e % 4] * mul * scale; });
+                    }
+                    if (far) {
+                        const int more = __float_as_int(sh.l[lane & 15][wave]);
+#pragma unroll
+                        for (int x = 0; x < U; ++x)
+#pragma unroll
+                            for (int e = 0; e < R; ++e) s[x][e] = __builtin_ldexpf(s[x][e], more);
                     }
                 } else
 #pragma unroll
