@@ -61,7 +61,7 @@ struct __align__(16) PagedShared {
 };
 
 constexpr int kJoin = 16;      // partial results that one workgroup joins at a time, all of their loads in flight together
-constexpr float kLeastUnit = -111.f;   // 8 bits: the smallest unit of weights, so that what brings them to it is a normal number
+constexpr int kLeastUnit = -110;       // 8 bits: the smallest unit of weights, so that what brings them to it and back is a normal number
 constexpr int kAgent = 16;     // buffer accesses at agent scope (past the XCD's own L2, like st_agent and ld_agent)
 
 // Activations as they lie in memory (A: float, or the bits of a 16-bit type) and as fp32.  The two are apart so that all loads are requested before the first conversion waits.
@@ -349,8 +349,9 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
         // the wave whose turn has the newest row rounds it as the pool does, and puts it into its page
         const bool fresh = a.k_new && c1 == chunks && (WAVES || (newest / P::TR & 3) == wave);
         float m = -INFINITY, l = 0.f;
-        // 8 bits: a weight goes into the products with its row's scale, w = exp2(score - m) * scale, in units of 2^(unit - 15) where 2^unit is the largest so far, as fp16 halves need it.
-        float unit_w = kLeastUnit;
+        // 8 bits: a weight goes into the products with its row's scale, w = exp2(score - m) * scale, in units of 2^(unit - 16) where 2^unit is more than the largest so far, as fp16 halves need it.  unit is a
+        // whole number: what brings sums from one to another is exact.
+        int unit_w = kLeastUnit;
         float new_ks = 0.f, new_vs = 0.f;
         f32x4 acc[ND];
 #pragma unroll
@@ -612,11 +613,16 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
 #pragma unroll
                     for (int e = 0; e < R; ++e) top = fmaxf(top, s[x][e]);
                 top = fmaxf(m, reduce_halves(reduce_row_pairs(top, MaxOp()), MaxOp()));
+                float kept = 1.f;                                   // 8 bits: what the sums keep, 1/2 to 1 times a power of two that goes to l and to the unit
                 if (__any(top > m)) {
-                    const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
-                    l *= f;
-                    if constexpr (P::ES == 1) unit_w -= top > m ? top - m : 0.f;
-                    else {
+                    if constexpr (P::ES == 1) {
+                        const float grown = m > -INFINITY ? fminf(top - m, 1e6f) : 0.f, whole = floorf(grown);
+                        kept = __builtin_amdgcn_exp2f(whole - grown);
+                        l = __builtin_ldexpf(l * kept, -(int)whole);
+                        unit_w -= (int)whole;
+                    } else {
+                        const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+                        l *= f;
 #pragma unroll
                         for (int d = 0; d < ND; ++d) acc[d] *= f;
                     }
@@ -641,15 +647,16 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                             most = fmaxf(most, fabsf(s[x][e]));
                         });
                     }
-                    most = __builtin_amdgcn_logf(reduce_halves(reduce_row_pairs(most, MaxOp()), MaxOp()));
-                    const float larger = fmaxf(fmaxf(unit_w, most), kLeastUnit);
-                    if (__any(larger > unit_w)) {
-                        const float f = __builtin_amdgcn_exp2f(unit_w - larger);       // (0 before the first row that counts: unit_w is -infinity then, and acc 0)
+                    most = reduce_halves(reduce_row_pairs(most, MaxOp()), MaxOp());
+                    // the largest weight becomes 65504 at most (fp16's largest) and 32752 at least
+                    const int larger = max(max(unit_w, most > 0.f ? __builtin_amdgcn_frexp_expf(most * (1.f + 0x1p-11f)) : kLeastUnit), kLeastUnit);
+                    if (__any(kept < 1.f || larger > unit_w)) {
+                        const float f = __builtin_ldexpf(kept, unit_w - larger);
 #pragma unroll
                         for (int d = 0; d < ND; ++d) acc[d] *= f;
                         unit_w = larger;
                     }
-                    const float by = __builtin_amdgcn_exp2f(15.f - unit_w);
+                    const float by = __builtin_ldexpf(1.f, 16 - unit_w);
 #pragma unroll
                     for (int x = 0; x < U; ++x)
 #pragma unroll
@@ -744,7 +751,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
             for (int more = turns; more > 1; --more) turn(std::true_type());
             turn(std::false_type());
             if constexpr (P::ES == 1) {
-                const float f = __builtin_amdgcn_exp2f(unit_w - 15.f);
+                const float f = __builtin_ldexpf(1.f, unit_w - 16);
 #pragma unroll
                 for (int d = 0; d < ND; ++d) acc[d] *= f;
             }

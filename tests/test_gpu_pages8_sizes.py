@@ -1,4 +1,4 @@
-"""Attention over pages of 8 bits where sizes are far from one: queries, keys and scales near the ends of fp32."""
+"""Attention over pages of 8 bits where sizes are far from one: queries, keys and scales near the ends of fp32, and weights whose unit follows a growing maximum."""
 import math
 
 import pytest
@@ -28,3 +28,48 @@ def test_scores_that_fp32_holds_are_right_whatever_they_are_made_of(kv, hd, keys
     out = cache.attend(0, q, scale=scale)
     used = torch.tensor(scale, dtype=torch.float32).double().item() or 1 / math.sqrt(hd)
     _check(out, *_reference(cache, q.double(), lens, scale=used))
+
+
+def _codes(values, kv):
+    """Bytes of codes that both types hold: 0 and powers of two up to 64."""
+    import torch
+    return values.to(torch.int8 if kv == "i8" else torch.float8_e4m3fn).view(torch.uint8)
+
+
+@pytest.mark.parametrize("kv", ["i8", "e4m3"])
+@pytest.mark.parametrize("exponent", [-90, -60, 0, 90])
+def test_sums_follow_a_growing_maximum_together(kv, exponent):
+    """Every value is c = 1.578125 * 2^exponent, so the output is c whatever the weights are, as long as the weights' sum and the weighted values' are scaled alike when the maximum grows.  One row of every 64
+    counts (the others have weights of 0), and its score is ahead of that of the row 256 before it by 0.004 to 0.3 (in powers of two), another step for each of 8192 heads; c is held as a code 2^k times a
+    scale c / 2^k, k from 0 to 6, so the largest weight times scale goes up and down by whole powers of two beside it.
+
+    4096 rows are 16 turns of each of a workgroup's four waves.  In a turn the weights' sum is multiplied (1 rounding) and gets a term (1), the values' sum is multiplied (1) and gets a weight's two halves
+    (2, each off by a step, 2 of 2^-24: 4): 7 of 2^-24.  A row is in the sums for 8 turns on average where the weights are alike, fewer where they grow: 56, and 64 with a fifth of the turns' weights apart.  A weight times its scale: 4
+    (2^-22); the waves' sums: the factor is the same for both, 2 * (1 + 3); the quotient: 3."""
+    import torch
+    from paper_2503_08524_amd import PagedCache
+    B, group, hd, n = 512, 16, 128, 4096
+    cache = PagedCache(group, 1, hd, n // 16, 16, B, n // 16, kv_dtype=kv, device=DEV)
+    cache.tables.copy_(torch.arange(n // 16, dtype=torch.int32, device=DEV).expand(B, -1))          # all sequences read the same pages
+    cache.rows.fill_(n)
+    c = 1.578125 * 2.0 ** exponent
+    row = torch.arange(n, device=DEV)
+    counts = row % 64 == 5
+    # keys: dim 0 alone, 64 times a scale that grows with the row, or -64 times a large one
+    k = torch.zeros(n, hd, device=DEV)
+    k[:, 0] = torch.where(counts, 64.0, -64.0)
+    ks = torch.where(counts, (row // 64 + 1).float(), 1e6)
+    two = 2.0 ** ((row // 64) * 5 % 7)
+    cache.k_pages.view(torch.uint8).copy_(_codes(k, kv).view(1, n // 16, 1, 16, hd))
+    cache.k_scales.copy_(ks.view(1, -1, 1, 16))
+    v = two[:, None].expand(n, hd).reshape(n // 16, 16, hd).transpose(1, 2).contiguous()            # [page][dim][row]
+    cache.v_pages.view(torch.uint8).copy_(_codes(v, kv).view(1, n // 16, 1, 1, hd, 16))
+    cache.v_scales.copy_((c / two).float().view(1, -1, 1, 16))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(exponent)
+    step = 0.004 + 0.296 * torch.rand(B, group, generator=g, device=DEV)
+    q = torch.zeros(B, group, hd, device=DEV)
+    q[:, :, 0] = step / (4 * 64 * math.log2(math.e))                                                # a step of four of the scale is `step` in powers of two
+    out = cache.attend(0, q, scale=1.0)
+    off = (out.double() / c - 1).abs()
+    assert float(off.max()) <= (64 + 4 + 8 + 3) * 2.0 ** -24, float(off.max()) * 2.0 ** 24
