@@ -22,6 +22,7 @@
 // runs a head, 9.2 us: lengths 0.4, place found 0.3, tables and q 1.4, rows 1.7, turn 0.7, merge 0.7, publish, arrive and join 2.4.
 #pragma once
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "codes8.h"
@@ -474,7 +475,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 }
             }
             // q as fp16 halves hi + lo, scaled by a power of two that puts its largest element at 2^14: 22 bits of it
-            float mul = (P::ES == 1 ? __builtin_amdgcn_frexp_mantf(a.scale) : a.scale) * 1.4426950408889634f;    // scores are kept in units of log2(e): every exponential is one hardware exp2
+            float mul = P::ES == 1 ? a.scale_part : a.scale * 1.4426950408889634f;    // scores are kept in units of log2(e): every exponential is one hardware exp2
             bool far = false;
             // In LDS from here on (where this wave puts its outputs in the end): in registers it would leave too few for the rows in flight.
             uint4* const q_lds = reinterpret_cast<uint4*>(sh.o[wave]) + lane;
@@ -504,7 +505,7 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                 if constexpr (P::ES == 1) {
                     // Codes have at most 2^31 in a product with q, and scales of rows 2^121: with 2^-120 to 2^95 ahead of the row's scale (all there is to it, but for queries or a scale far from one) mul is a normal
                     // number and only a score that is too large for fp32 overflows.  The rest, `far`, goes by head into LDS, where sums come at the end, and is left out where no head has any.
-                    const int all = __builtin_amdgcn_frexp_expf(a.scale) - ex, near = min(max(all, -120), 95);
+                    const int all = a.scale_exp - ex, near = min(max(all, -120), 95);
                     mul = __builtin_ldexpf(mul, near);
                     far = __any(all != near);
                     if (g == 0) sh.l[i][wave] = __int_as_float(all - near);
@@ -614,18 +615,17 @@ __device__ __forceinline__ void attn_paged_runs(const PagedAttnArgs& a, PagedSha
                     for (int e = 0; e < R; ++e) top = fmaxf(top, s[x][e]);
                 top = fmaxf(m, reduce_halves(reduce_row_pairs(top, MaxOp()), MaxOp()));
                 float kept = 1.f;                                   // 8 bits: what the sums keep, 1/2 to 1 times a power of two that goes to l and to the unit
-                if (__any(top > m)) {
-                    if constexpr (P::ES == 1) {
-                        const float grown = m > -INFINITY ? fminf(top - m, 1e6f) : 0.f, whole = floorf(grown);
-                        kept = __builtin_amdgcn_exp2f(whole - grown);
-                        l = __builtin_ldexpf(l * kept, -(int)whole);
-                        unit_w -= (int)whole;
-                    } else {
-                        const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
-                        l *= f;
+                if constexpr (P::ES == 1) {                         // (beside the exponentials, without a branch of its own)
+                    const float grown = m > -INFINITY ? fminf(top - m, 1e6f) : 0.f, whole = floorf(grown);
+                    kept = __builtin_amdgcn_exp2f(whole - grown);
+                    l = __builtin_ldexpf(l * kept, -(int)whole);
+                    unit_w -= (int)whole;
+                    m = top;
+                } else if (__any(top > m)) {
+                    const float f = top > m ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+                    l *= f;
 #pragma unroll
-                        for (int d = 0; d < ND; ++d) acc[d] *= f;
-                    }
+                    for (int d = 0; d < ND; ++d) acc[d] *= f;
                     m = top;
                 }
                 const float sub = m > -INFINITY ? m - P::SHIFT : 0.f;
@@ -964,7 +964,7 @@ template <typename T, int HD, typename A, bool MANY>
 __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedAttnArgs a) {
     __shared__ PagedShared<T, HD> sh;
     paged_take_args(a);
-    if constexpr (sizeof(T) == 1) asm volatile("" :: "s"(a.k_scales), "s"(a.v_scales));
+    if constexpr (sizeof(T) == 1) asm volatile("" :: "s"(a.k_scales), "s"(a.v_scales), "s"(a.scale_part), "s"(a.scale_exp));
     auto length = [&](int b) { return min(max(a.rows[b], 0), a.max_rows); };
     const Lengths n = take_lengths<PagedShape<T, HD>>(a.B, threadIdx.x & 63, length);
     if constexpr (MANY) {
@@ -987,6 +987,7 @@ int launch(PagedAttnArgs a, int n_cu, hipStream_t s) {
     const int resident = std::min(2 * n_cu, kPagedMaxWgs), n = (int)std::min<long long>(most, resident);
     a.by_runs = Divisor(n);
     a.by_waves = Divisor(4 * n);
+    a.scale_part = std::frexp(a.scale, &a.scale_exp) * 1.4426950408889634f;
     return heads >= nearly(4 * resident) ? launch_many<T, HD, true>(a, n, s) : launch_many<T, HD, false>(a, n, s);
 }
 

@@ -93,6 +93,8 @@ struct PagedAttnArgs {
     int* tickets;                          // [B][H_kv * tiles], then [2 * runs], zero between launches
     Divisor by_runs, by_waves;             // set by launch_attention_paged: its workgroups and their waves
     float *k_scales, *v_scales;            // this layer's scales of 8-bit rows (last: ahead of what every launch takes they cost the others 0.2 us of 9)
+    float scale_part;                      // scale log2(e) = scale_part * 2^scale_exp, set by launch_attention_paged8
+    int scale_exp;
 };
 int launch_attention_paged(const PagedAttnArgs& a, int hd, int kv_dtype, int n_cu, hipStream_t s);
 int launch_attention_paged8(const PagedAttnArgs& a, int hd, int kv_dtype, int n_cu, hipStream_t s);    // D3_I8, D3_E4M3

@@ -26,6 +26,7 @@ def test_scores_that_fp32_holds_are_right_whatever_they_are_made_of(kv, hd, keys
     cache.k_scales.mul_(keys)
     q = (torch.empty(3, 4, hd, dtype=torch.float64, device=DEV).normal_(generator=g) * queries).float()
     out = cache.attend(0, q, scale=scale)
+    assert out.isfinite().all()                             # (which _check does not ask)
     used = torch.tensor(scale, dtype=torch.float32).double().item() or 1 / math.sqrt(hd)
     _check(out, *_reference(cache, q.double(), lens, scale=used))
 
