@@ -291,7 +291,7 @@ int d3_pages_append(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n,
                     int64_t token_stride, int64_t head_stride, int64_t layer_stride, const float *rope_cs, void *hip_stream);
 
 /* The other way round: rows `slots` of `n_layers` layers from `layer` on, as the pools hold them (keys as they were turned), into k, v: dev [n_layers][n][H_kv][head_dim] of `dtype` (D3_F32, D3_BF16 or D3_F16), by
- * the strides of d3_pages_append.  From pools of 8 bits code * scale is rounded to fp32, then to `dtype`; from the others the value once.  Rows of slots outside the pool are left as they are; a slot may be listed
+ * the strides of d3_pages_append, by which no two rows of k and v may lie on each other (in the order of the strides each passes over all that the ones before it span; k is not v).  From pools of 8 bits code * scale is rounded to fp32, then to `dtype`; from the others the value once.  Rows of slots outside the pool are left as they are; a slot may be listed
  * more than once.  n at most 2^28. */
 int d3_pages_read(d3_pages *pages, int32_t layer, int32_t n_layers, int32_t n, const int32_t *slots, void *k, void *v, int32_t dtype, int64_t token_stride, int64_t head_stride, int64_t layer_stride, void *hip_stream);
 

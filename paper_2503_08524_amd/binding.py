@@ -470,7 +470,7 @@ class PagedCache:
 
     def read(self, layer: int, slots, k=None, v=None, dtype=None, n_layers: Optional[int] = None):
         """The rows `slots` (int32 CUDA tensor [n]) as the pools hold them, keys as they were turned: into k, v [n][n_kv_heads][head_dim], or [m][n][n_kv_heads][head_dim] of the m layers from
-        `layer` on, which have the same strides, the last dim dense, and are returned.  Rows of slots outside the pools are left as they are.  Where k and v are left out they are made, of `dtype`
+        `layer` on, which have the same strides, the last dim dense, no two rows on each other, and are returned.  Rows of slots outside the pools are left as they are.  Where k and v are left out they are made, of `dtype`
         (float32 if that is left out too), for n_layers layers, or without that dim for one; rows of slots outside the pools are then 0."""
         if k is None and v is None:
             dims = (slots.numel(), self.n_kv_heads, self.head_dim) if n_layers is None else (n_layers, slots.numel(), self.n_kv_heads, self.head_dim)

@@ -5,6 +5,7 @@
 
 #include "d3_error.h"
 #include "pages.h"
+#include "strided.h"
 
 using namespace d3;
 
@@ -216,6 +217,10 @@ extern "C" int d3_pages_read(d3_pages* pages, int32_t layer, int32_t n_layers, i
     if (!aligned16(k) || !aligned16(v) || token_stride % unit != 0 || head_stride % unit != 0 || layer_stride % unit != 0)
         return fail(D3_EINVAL, "d3_pages_read: k, v and their strides must be multiples of 16 bytes");
     const d3_pages_desc& d = pages->desc;
+    const intptr_t apart = (reinterpret_cast<intptr_t>(v) - reinterpret_cast<intptr_t>(k)) / elem_bytes(dtype);
+    if (apart == 0 || rows_overlap(d.head_dim, {{n, token_stride}, {d.n_kv_heads, head_stride}, {n_layers, layer_stride}}, apart))
+        return fail(D3_EINVAL, "d3_pages_read: rows of k and v must not lie on each other (strides of row, head and layer %lld, %lld, %lld, v %lld elements behind k)", (long long)token_stride, (long long)head_stride,
+                    (long long)layer_stride, (long long)apart);
     ReadArgs a{};
     a.n = n; a.n_layers = n_layers; a.H_kv = d.n_kv_heads; a.hd = d.head_dim; a.page_shift = __builtin_ctz(d.page_rows); a.n_slots = pages->n_slots();
     a.slots = slots; a.k = k; a.v = v; a.dtype = dtype;
