@@ -82,15 +82,15 @@ int check_dtype(const char* who, int32_t dtype) {
 
 namespace {
 // Compute units of a gfx950 device, asked once per device (the properties take longer than the rest of d3_pages_create).
-int device_cus(int dev, int* n_cu) {
+int device_cus(const char* who, int dev, int* n_cu) {
     constexpr int kMaxDevices = 64;
     static std::atomic<int> known[kMaxDevices];
-    if (dev < 0 || dev >= kMaxDevices) return fail(D3_EDEVICE, "d3_pages_create: device index %d is outside [0, %d)", dev, kMaxDevices);
+    if (dev < 0 || dev >= kMaxDevices) return fail(D3_EDEVICE, "%s: device index %d is outside [0, %d)", who, dev, kMaxDevices);
     *n_cu = known[dev].load(std::memory_order_relaxed);
     if (*n_cu > 0) return D3_OK;
     hipDeviceProp_t prop;
     D3_HIP(hipGetDeviceProperties(&prop, dev));
-    if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return fail(D3_EDEVICE, "d3_pages_create: built for gfx950, device is %s", prop.gcnArchName);
+    if (strncmp(prop.gcnArchName, "gfx950", 6) != 0) return fail(D3_EDEVICE, "%s: built for gfx950, device is %s", who, prop.gcnArchName);
     *n_cu = prop.multiProcessorCount;
     known[dev].store(*n_cu, std::memory_order_relaxed);
     return D3_OK;
@@ -104,18 +104,18 @@ extern "C" size_t d3_pages_workspace_size(const d3_pages_desc* desc) {
 }
 
 namespace {
-int create(d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pages, float* k_scales, float* v_scales, void* workspace, size_t workspace_bytes) {
-    if (!k_pages || !v_pages || !workspace) return fail(D3_EINVAL, "d3_pages_create: pool or workspace is NULL");
-    if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(D3_EINVAL, "d3_pages_create: the pools must be 16-byte aligned");
-    if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(D3_EINVAL, "d3_pages_create: workspace must be %zu-byte aligned", kAlign);
+int create(const char* who, d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pages, float* k_scales, float* v_scales, void* workspace, size_t workspace_bytes) {
+    if (!k_pages || !v_pages || !workspace) return fail(D3_EINVAL, "%s: pool or workspace is NULL", who);
+    if (!aligned16(k_pages) || !aligned16(v_pages)) return fail(D3_EINVAL, "%s: the pools must be 16-byte aligned", who);
+    if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0) return fail(D3_EINVAL, "%s: workspace must be %zu-byte aligned", who, kAlign);
     size_t part_ml, tickets;
     const size_t need = layout(*desc, &part_ml, &tickets);
-    if (workspace_bytes < need) return fail(D3_EINVAL, "d3_pages_create: workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    if (workspace_bytes < need) return fail(D3_EINVAL, "%s: workspace has %zu bytes, %zu needed", who, workspace_bytes, need);
     int dev = 0, n_cu = 0;
     D3_HIP(hipGetDevice(&dev));
-    D3_CHECK(device_cus(dev, &n_cu));
+    D3_CHECK(device_cus(who, dev, &n_cu));
     d3_pages* p = new (std::nothrow) d3_pages();
-    if (!p) return fail(D3_EINVAL, "d3_pages_create: out of host memory");
+    if (!p) return fail(D3_EINVAL, "%s: out of host memory", who);
     p->desc = *desc;
     p->k = static_cast<char*>(k_pages); p->v = static_cast<char*>(v_pages); p->ws = static_cast<char*>(workspace);
     p->ks = k_scales; p->vs = v_scales;
@@ -123,7 +123,7 @@ int create(d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pag
     p->part_ml = part_ml; p->tickets = tickets;
     hipError_t e = hipMemset(p->ws + tickets, 0, need - tickets);              // arrival counters start at 0
     if (e == hipSuccess) e = hipStreamSynchronize(nullptr);                   // calls may come on any stream
-    if (e != hipSuccess) { delete p; return fail(D3_EDEVICE, "d3_pages_create: hipMemset failed: %s", hipGetErrorString(e)); }
+    if (e != hipSuccess) { delete p; return fail(D3_EDEVICE, "%s: hipMemset failed: %s", who, hipGetErrorString(e)); }
     *out = p;
     return D3_OK;
 }
@@ -134,7 +134,7 @@ extern "C" int d3_pages_create(d3_pages** out, const d3_pages_desc* desc, void* 
     *out = nullptr;
     D3_CHECK(check_desc(desc));
     if (kv_elem_bytes(desc->kv_dtype) == 1) return fail(D3_EINVAL, "d3_pages_create: pools of 8 bits have scales (d3_pages_create_scaled)");
-    return create(out, desc, k_pages, v_pages, nullptr, nullptr, workspace, workspace_bytes);
+    return create("d3_pages_create", out, desc, k_pages, v_pages, nullptr, nullptr, workspace, workspace_bytes);
 }
 
 extern "C" int d3_pages_create_scaled(d3_pages** out, const d3_pages_desc* desc, void* k_pages, void* v_pages, float* k_scales, float* v_scales, void* workspace, size_t workspace_bytes) {
@@ -144,7 +144,7 @@ extern "C" int d3_pages_create_scaled(d3_pages** out, const d3_pages_desc* desc,
     if (kv_elem_bytes(desc->kv_dtype) != 1) return fail(D3_EINVAL, "d3_pages_create_scaled: only pools of 8 bits (D3_I8, D3_E4M3) have scales (d3_pages_create)");
     if (!k_scales || !v_scales) return fail(D3_EINVAL, "d3_pages_create_scaled: scales are NULL");
     if (!aligned16(k_scales) || !aligned16(v_scales)) return fail(D3_EINVAL, "d3_pages_create_scaled: the scales must be 16-byte aligned");
-    return create(out, desc, k_pages, v_pages, k_scales, v_scales, workspace, workspace_bytes);
+    return create("d3_pages_create_scaled", out, desc, k_pages, v_pages, k_scales, v_scales, workspace, workspace_bytes);
 }
 
 extern "C" int d3_pages_destroy(d3_pages* pages) {
