@@ -139,7 +139,10 @@ def d3_plan_from_table(L: int, keep, drop_begin):
 
 
 def _desc(shape, kv_dtype: str, max_batch: int, max_seq: int) -> _ModelDesc:
-    dt = {"f32": D3_F32, "bf16": D3_BF16, "f16": D3_F16}
+    dt = {"f32": D3_F32, "bf16": D3_BF16, "f16": D3_F16, "i8": D3_I8, "e4m3": D3_E4M3}         # (the library says which of them a context's weights and cache may have)
+    for name, kind in (("the shape's dtype", shape.dtype), ("kv_dtype", kv_dtype)):
+        if kind not in dt:
+            raise ValueError(f"{name} must be one of {sorted(dt)} (got {kind!r})")
     return _ModelDesc(shape.L, shape.d, shape.H, shape.H_kv, shape.hd, shape.F, shape.V, float(shape.eps),
                       float(shape.rope_base), dt[shape.dtype], dt[kv_dtype], max_batch, max_seq)
 

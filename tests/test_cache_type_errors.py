@@ -1,9 +1,10 @@
-"""What a caller is told who hands a wrong pointer to a handle of pages (host checks, no GPU)."""
+"""What a caller is told who asks for a cache type that is not offered, or hands a wrong pointer to a pool of 8 bits (host checks, no GPU)."""
 import ctypes as C
 
 import numpy as np
 import pytest
 
+import d3_inputs
 import paper_2503_08524_amd as d3
 from paper_2503_08524_amd import binding
 from paper_2503_08524_amd import build as d3_build
@@ -14,6 +15,27 @@ def lib():
     if d3_build.is_stale():
         d3_build.build()
     return d3.load_library()
+
+
+@pytest.mark.parametrize("kv,code", [("i8", binding.D3_I8), ("e4m3", binding.D3_E4M3)])
+def test_a_context_with_a_cache_of_8_bits_is_refused_by_name(lib, kv, code):
+    with pytest.raises(d3.D3Error) as e:
+        binding.Decoder(d3_inputs.TINY, {}, 1, 64, kv_dtype=kv)
+    assert "kv_dtype must be D3_F32 or D3_F16" in str(e.value)
+    assert binding.d3_workspace_size(d3_inputs.TINY, kv, 1, 64) == 0
+    desc, out = binding._desc(d3_inputs.TINY, kv, 1, 64), C.c_void_p()
+    assert desc.kv_dtype == code
+    room = np.zeros(4096, np.uint8).ctypes.data
+    assert lib.d3_create(C.byref(out), C.byref(desc), C.byref(binding._Weights()), room, room, room, 1 << 20) == -1
+    assert "kv_dtype must be D3_F32 or D3_F16" in lib.d3_last_error().decode() and out.value is None
+
+
+def test_a_type_that_is_none_is_a_value_error_that_names_them(lib):
+    for kv in ("fp16", "int8", "F32"):
+        for make in (lambda: binding.Decoder(d3_inputs.TINY, {}, 1, 64, kv_dtype=kv), lambda: binding.d3_workspace_size(d3_inputs.TINY, kv, 1, 64)):
+            with pytest.raises(ValueError) as e:
+                make()
+            assert "kv_dtype" in str(e.value) and "'f16'" in str(e.value)
 
 
 @pytest.mark.parametrize("entry,kind", [("d3_pages_create", binding.D3_F16), ("d3_pages_create_scaled", binding.D3_I8)])
