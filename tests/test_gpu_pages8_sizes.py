@@ -3,7 +3,7 @@ import math
 
 import pytest
 
-from tests.test_gpu_pages8 import _cache, _check, _reference
+from tests.test_gpu_pages8 import CASES, _angles, _cache, _check, _reference, _slots, _state, _types, _values
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,46 @@ def test_sums_follow_a_growing_maximum_together(kv, exponent):
     out = cache.attend(0, q, scale=1.0)
     off = (out.double() / c - 1).abs()
     assert float(off.max()) <= (64 + 4 + 8 + 3) * 2.0 ** -24, float(off.max()) * 2.0 ** 24
+
+
+@pytest.mark.parametrize("kv", ["i8", "e4m3"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("keys,queries", [(1.0, 1e4), (1e3, 30.0), (1e33, 1.0), (1e36, 1.0), (1e-30, 3e37)])
+def test_far_scores_pick_their_rows(kv, hd, keys, queries):
+    """Scores so far apart that a head takes one row, or the few whose scores are nearest to the largest.  With E what a score may be off (the suite's bound), rows 2 E + 30 behind the largest weigh
+    e^-30 of it at most, so every dim of an output lies between the smallest and the largest value of the rows that are nearer, but for that and the sums' roundings; where that is one row, it is its value."""
+    import torch
+    lens = [70, 300, 1000, 64, 65, 129, 500, 33]
+    cache, g = _cache(lens, 2, 2, hd, kv, 16, seed=23, garbage=True)
+    cache.k_scales.mul_(keys)
+    q = torch.empty(len(lens), 4, hd, device=DEV).normal_(generator=g) * queries
+    out = cache.attend(0, q).double()
+    assert out.isfinite().all()
+    state = _state(cache)
+    K, V = (_values(state[i][0], state[2 + i][0], kv) for i in range(2))
+    alone = 0
+    for b, n in enumerate(lens):
+        at = _slots(cache, b, range(n))
+        k, v = K[at].repeat_interleave(2, 1), V[at].repeat_interleave(2, 1)
+        x = q[b].double()
+        score = (x * k).sum(-1).T / math.sqrt(hd)                                                   # [head][row]
+        size = (x.abs() * k.abs()).sum(-1).T.amax(-1) / math.sqrt(hd)
+        near = score >= (score.amax(-1) - 2 * (2.0 ** -22 + (hd + 6) * 2.0 ** -24) * size - 30)[:, None]
+        lo, hi = (getattr(torch.where(near.T[..., None], v, sign * math.inf), end)(0) for sign, end in ((1, "amin"), (-1, "amax")))
+        slack = v.abs().amax(0) * (3 * 2.0 ** -22 + (n / 8 + 64) * 2.0 ** -24 + n * math.exp(-30))
+        assert ((out[b] >= lo - slack) & (out[b] <= hi + slack)).all()
+        alone += int((near.sum(-1) == 1).sum())
+    assert alone >= 0.8 * 4 * len(lens)
+
+
+@pytest.mark.parametrize("case", range(len(CASES)))
+def test_outputs_are_numbers(case):
+    """Of every case that is compared with 64 bits elsewhere, by bounds that a NaN passes."""
+    import torch
+    lens, heads, group, hd, kv, act, page_rows, new, rope = CASES[case]
+    cache, g = _cache(lens, heads, group, hd, kv, page_rows, seed=case, garbage=True)
+    t = _types()[act]
+    q = torch.empty(len(lens), heads * group, hd, dtype=t, device=DEV).normal_(generator=g)
+    k, v = (torch.empty(len(lens), heads, hd, dtype=t, device=DEV).normal_(generator=g) for _ in range(2))
+    cs = _angles([max(n - 1, 0) for n in lens], hd) if rope else None
+    assert cache.attend(0, q, k if new else None, v if new else None, rope_cs=cs).isfinite().all()
