@@ -305,7 +305,7 @@ int d3_pages_live(d3_pages *pages, int32_t B, const int32_t *rows, const int32_t
  * The call cannot tell a sequence that a reserve refused, or that asked for nothing: it would lose its newest row, so `rows` is then d3_pages_live's.  rope_cs: dev float [B][head_dim / 2][2]: q and
  * k_new turn by it; NULL: neither does.  q, k_new, v_new, rope_cs 16-byte aligned, q_stride and kv_stride multiples of 16 bytes.  scale: 0 for 1 / sqrt(head_dim).
  * out may be q itself.  Keys and values are used as the pool holds them; sums, maxima and partial results are in 32 bits.  Into the products q and the weights go in fp32 with D3_F32 pools, as
- * the sum of two fp16 halves (22 bits) with D3_F16 pools and those of 8 bits, where a weight is multiplied by its row's scale first; the halves of these products count in steps of 2^-40 of the largest so far.  A row whose score is -infinity has the weight 0; out is 0 too where every row's is. */
+ * the sum of two fp16 halves (22 bits) with D3_F16 pools and those of 8 bits, where a weight is multiplied by its row's scale first; the halves of these products count in steps of 2^-39 of the largest so far (2^-40 off at most).  A row whose score is -infinity has the weight 0; out is 0 too where every row's is. */
 int d3_pages_attention(d3_pages *pages, int32_t layer, int32_t B, const void *q, const void *k_new, const void *v_new, int32_t dtype, int64_t q_stride,
                        int64_t kv_stride, const float *rope_cs, const int32_t *tables, const int32_t *rows, float scale, void *out,
                        int64_t out_stride, void *hip_stream);

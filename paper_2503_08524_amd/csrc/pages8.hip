@@ -146,7 +146,7 @@ struct Units {
 // A key is a row of its page: 16 bytes of the source's lower half and their partners per thread, the row's magnitude from the threads beside it.
 // Values: a wave has 16 tokens, a lane one or two dims of all of them; where 16 tokens fill a unit of 16 rows it writes the unit's 16 bytes per dim, elsewhere bytes.
 // Workgroups of 16 / 32 / 64 tokens, us (the shortest of 30 launches): 512 rows of 32 heads, fp32 to e4m3 with rotation, 10.7 / 8.3 / 7.1; 8 layers x 1024 rows of 8 heads 26.0 / 24.1 / 17.8 (4.7 TB/s, a large copy's rate); 1024 rows of 40 heads,
-// fp16 to i8, 15.8 / 12.8 / 10.5; read, 4 layers x 2304 rows of 32 heads, i8 to fp16, 55 / 47 / 40 (5.7 TB/s): workgroups begin one after the other, and the loads of four rounds are in flight together.
+// fp16 to i8, 15.8 / 12.8 / 10.5; read, 4 layers x 2304 rows of 32 heads, i8 to fp16, 55 / 47 / 40 (the first of a series, 5.7 TB/s; from the third on 46 to 48, 4.8 TB/s: the 151 MB that the one before has written are then presumably still on their way from the memory-side cache): workgroups begin one after the other, and the loads of four rounds are in flight together.
 constexpr int kTokens = 64, kValueTokens = kTokens / 4;
 
 template <typename S, typename T, int HD>
